@@ -339,6 +339,64 @@ int cephalo_op_attention_bwd(const cephalo_layer_desc* desc, const void* qkv, co
                              const float* lse, float* dvec, void* dqkv, int32_t micro_batch, void* stream);
 
 /* ---------------------------------------------------------------------------------------
+ * Packed samples: documents or images of different lengths that lie one behind the other in the rows of one micro-batch,
+ * sample i in rows [starts[i], starts[i+1]).  The packed projection qkv [tokens, qkv_pitch] holds in each row `heads`
+ * queries, then `kv_heads` keys, then `kv_heads` values of head_dim columns; query head a reads key head
+ * a / (heads / kv_heads), so that kv_heads = heads is the form above and kv_heads = 1 shares one key head.
+ * Attention stays inside a sample: query row q of it sees its rows t <= q (causal) or all of them.  Samples may have any
+ * length, 0 and 1 too.  No sample's values reach another's results, not-a-numbers and infinities included.  Rows that belong
+ * to no sample are neither read nor written, and neither are columns past a row's width. */
+typedef struct cephalo_packed_desc {
+  int32_t heads, kv_heads;   /* heads is a multiple of kv_heads */
+  int32_t head_dim;          /* up to 128, in BF16 mode a multiple of 8 */
+  int32_t causal;            /* 0 or 1 */
+  int32_t dtype;             /* CEPHALO_F32 or CEPHALO_BF16 */
+  float   scale;             /* of the scores; 0: 1/sqrt(head_dim) */
+  int64_t tokens;            /* rows of qkv, O, dO and dqkv, columns of lse; below 2^31 */
+  int64_t qkv_pitch, o_pitch;/* elements from one row of qkv (dqkv) and of O (dO) to the next; in BF16 mode multiples of 8 */
+  int32_t samples, longest, tiles;   /* written by cephalo_packed_plan */
+} cephalo_packed_desc;
+
+/* The work list of a set of samples, made once for all layers and passes that run on them.  Host work only: starts [samples + 1]
+ * (not decreasing, inside [0, tokens]) is host memory, and so is `plan`, at least cephalo_packed_plan_bytes(samples, tokens)
+ * bytes; the caller copies its first 16 * desc->tiles bytes to the device, where the calls below take it.  Fills samples, longest and
+ * tiles of the desc.  A list depends on `causal` and on the starts alone. */
+size_t cephalo_packed_plan_bytes(int32_t samples, int64_t tokens);
+int cephalo_packed_plan(cephalo_packed_desc* desc, int32_t samples, const int32_t* starts, void* plan, size_t plan_bytes);
+
+/* Forward: O [tokens, o_pitch] and lse [heads, tokens] fp32, the log-sum-exp of each query row's scaled, masked scores.
+ * Backward: dqkv [tokens, qkv_pitch] from dO and what the forward wrote; the sums over the query heads that share a key head are formed
+ * in 32 bits, in a fixed order (reproducible).  workspace: device, cephalo_op_attention_packed_bwd_workspace(desc) bytes (0: a desc
+ * that the calls refuse); no two calls that overlap in time may share it.  plan, qkv, O, dO, lse, dqkv: device, 16-byte aligned. */
+int cephalo_op_attention_packed_fwd(const cephalo_packed_desc* desc, const void* plan, const void* qkv, void* O, float* lse, void* stream);
+size_t cephalo_op_attention_packed_bwd_workspace(const cephalo_packed_desc* desc);
+int cephalo_op_attention_packed_bwd(const cephalo_packed_desc* desc, const void* plan, const void* qkv, const void* O, const void* dO,
+                                    const float* lse, void* dqkv, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Rotary positions with several axes (time, height, width of a patch; one axis: the place in a text): `heads` heads of head_dim
+ * columns, next to one another in each of `rows` rows, are turned.  Axis k owns the next axis_dims[k] columns of a head (even,
+ * 0 allowed; together at most head_dim, columns past them are copied), and pair (2i, 2i+1) of them turns by
+ *   positions[row][k] * base^(-2i / axis_dims[k]),   inverse: by the negative angle (the gradient's way back).
+ * positions: device int32 [rows, axes]; axis_dims: HOST [axes], axes 1 to 8.  The angle is formed in 64 bits.  src and dst (device, pitches in elements) may be
+ * the same buffer with the same pitch; they must not overlap otherwise.  Queries and keys of the packed projection are neighbours: heads + kv_heads
+ * heads in one call.  head_dim: up to 128, a multiple of 8 (BF16) or 4 (F32), and so are the pitches. */
+int cephalo_op_rotary_axes(int32_t dtype, const void* src, int64_t src_pitch, void* dst, int64_t dst_pitch, const int32_t* positions, int64_t rows,
+                           int32_t axes, const int32_t* axis_dims, int32_t heads, int32_t head_dim, double base, int32_t inverse, void* stream);
+
+/* Dropout of a branch where it joins the residual stream, with a mask that is drawn and never stored:
+ *   add:  out[i] = resid[i] + (keep_i ? branch[i] * scale : 0)        bwd:  dbranch[i] = keep_i ? dy[i] * scale : 0
+ * (the gradient of resid is dy itself).  keep_i: 16-bit word first + i of the stream of `seed` is at least round(65536 p); scale = 65536 / (65536 - round(65536 p)).
+ * Words 8j .. 8j+7 of a stream are the four results of Philox4x32-10 (Salmon et al., 2011) for counter j and key seed, the low half of each first.  An
+ * element's word depends on its place alone: calls on parts of a tensor, each with its own `first`, drop what one call drops.
+ *   branch, dbranch  device, n in dtype;  resid, out, dy  device, n fp32; out may be resid
+ *   p                in [0, 1), a multiple of 2^-16 after rounding;  first: a multiple of 8
+ *   counter          device, one 64-bit word that is added to `first` when the kernel runs (a multiple of 8: it is rounded down), or NULL.  A captured
+ *                    graph draws new words at each replay if the caller advances it between them. */
+int cephalo_op_dropout_add(int32_t dtype, const void* branch, const float* resid, float* out, int64_t n, float p, uint64_t seed, int64_t first,
+                           const uint64_t* counter, void* stream);
+int cephalo_op_dropout_bwd(int32_t dtype, const float* dy, void* dbranch, int64_t n, float p, uint64_t seed, int64_t first, const uint64_t* counter, void* stream);
+
+/* ---------------------------------------------------------------------------------------
  * A whole stack on one GPU's batch share, in the layered order of Sec. 3.2 ("Layered Gradient
  * Accumulation": all micro-batches pass through a layer before the next layer, forward and backward).
  * The paper trains such models (Table 2) without describing their pieces; the form here: learned token

@@ -60,8 +60,22 @@ class ClusterModel(ctypes.Structure):
                 ("mem_base", ctypes.c_double), ("mem_per_sample", ctypes.c_double), ("state_bytes", ctypes.c_double)]
 
 
+class PackedDesc(ctypes.Structure):
+    _fields_ = [("heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("causal", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("scale", ctypes.c_float), ("tokens", ctypes.c_int64), ("qkv_pitch", ctypes.c_int64), ("o_pitch", ctypes.c_int64),
+                ("samples", ctypes.c_int32), ("longest", ctypes.c_int32), ("tiles", ctypes.c_int32)]
+
+
+def packed_desc(heads, kv_heads, head_dim, causal, dtype, tokens, qkv_pitch=None, o_pitch=None, scale=0.0):
+    """The pitches default to rows without gaps."""
+    return PackedDesc(int(heads), int(kv_heads), int(head_dim), int(causal), int(dtype), float(scale), int(tokens),
+                      int((heads + 2 * kv_heads) * head_dim if qkv_pitch is None else qkv_pitch), int(heads * head_dim if o_pitch is None else o_pitch), 0, 0, 0)
+
+
 _vp, _i32, _i64, _f32, _sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float, ctypes.c_size_t
 _dp = ctypes.POINTER(LayerDesc)
+_pp = ctypes.POINTER(PackedDesc)
+_u64 = ctypes.c_uint64
 
 # name -> (restype, argtypes); must list every symbol include/cephalo.h declares
 SIGNATURES = {
@@ -121,6 +135,14 @@ SIGNATURES = {
                                           ctypes.POINTER(ctypes.c_double)]),
     "cephalo_plan_units": (ctypes.c_int, [_i32, ctypes.POINTER(ctypes.c_double), _i32, ctypes.c_int64, ctypes.POINTER(ctypes.c_int64),
                                           ctypes.POINTER(ctypes.c_int64), ctypes.POINTER(_i32)]),
+    "cephalo_packed_plan_bytes": (_sz, [_i32, _i64]),
+    "cephalo_packed_plan": (ctypes.c_int, [_pp, _i32, ctypes.POINTER(_i32), _vp, _sz]),
+    "cephalo_op_attention_packed_fwd": (ctypes.c_int, [_pp, _vp, _vp, _vp, _vp, _vp]),
+    "cephalo_op_attention_packed_bwd_workspace": (_sz, [_pp]),
+    "cephalo_op_attention_packed_bwd": (ctypes.c_int, [_pp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "cephalo_op_rotary_axes": (ctypes.c_int, [_i32, _vp, _i64, _vp, _i64, _vp, _i64, _i32, ctypes.POINTER(_i32), _i32, _i32, ctypes.c_double, _i32, _vp]),
+    "cephalo_op_dropout_add": (ctypes.c_int, [_i32, _vp, _vp, _vp, _i64, _f32, _u64, _i64, _vp, _vp]),
+    "cephalo_op_dropout_bwd": (ctypes.c_int, [_i32, _vp, _vp, _i64, _f32, _u64, _i64, _vp, _vp]),
     "cephalo_op_attention_fwd": (ctypes.c_int, [_dp, _vp, _vp, _vp, _i32, _vp]),
     "cephalo_op_attention_bwd": (ctypes.c_int, [_dp, _vp, _vp, _vp, _vp, _vp, _vp, _i32, _vp]),
 }
@@ -386,6 +408,71 @@ def cephalo_op_attention_fwd(desc, qkv, O, lse, micro_batch, stream=None):
 def cephalo_op_attention_bwd(desc, qkv, O, dO, lse, dvec, dqkv, micro_batch, stream=None):
     _check(lib().cephalo_op_attention_bwd(ctypes.byref(desc), _ptr(qkv), _ptr(O), _ptr(dO), _ptr(lse), _ptr(dvec),
                                           _ptr(dqkv), micro_batch, _stream(stream)))
+
+
+def _buffer(what, t, dtype, elements):
+    """The address of a device tensor of at least so many elements of that type (dtype: a torch type, or the library's F32 or BF16)."""
+    want = {F32: torch.float32, BF16: torch.bfloat16}.get(dtype, dtype)
+    if t.dtype != want or t.numel() < elements:
+        raise CephaloError("%s: expected %d elements of %s, got %d of %s" % (what, elements, want, t.numel(), t.dtype))
+    if t.is_cuda and t.device.index != torch.cuda.current_device():
+        raise CephaloError("%s: on %s, but the current device is %d" % (what, t.device, torch.cuda.current_device()))
+    return _ptr(t)
+
+
+def cephalo_packed_plan(desc, starts):
+    """The work list of the samples (rows starts[i] to starts[i + 1]), an int32 host tensor to copy to the device; fills the desc."""
+    starts = [int(v) for v in starts]
+    size = int(lib().cephalo_packed_plan_bytes(len(starts) - 1, desc.tokens))
+    plan = torch.zeros(max(size, 16) // 16, 4, dtype=torch.int32)
+    _check(lib().cephalo_packed_plan(ctypes.byref(desc), len(starts) - 1, _ints(starts), plan.data_ptr(), plan.numel() * 4))
+    return plan[:max(desc.tiles, 1)].clone()
+
+
+def _packed_buffers(desc, plan, qkv, O, lse):
+    rows = max(desc.tokens - 1, 0)
+    width = desc.heads * desc.head_dim
+    of_qkv, of_o = rows * desc.qkv_pitch + width + 2 * desc.kv_heads * desc.head_dim, rows * desc.o_pitch + width
+    return (_buffer("plan", plan, torch.int32, 4 * desc.tiles), of_qkv, of_o, _buffer("qkv", qkv, desc.dtype, of_qkv), _buffer("O", O, desc.dtype, of_o),
+            _buffer("lse", lse, torch.float32, desc.heads * desc.tokens))
+
+
+def cephalo_op_attention_packed_fwd(desc, plan, qkv, O, lse, stream=None):
+    plan, _, _, qkv, O, lse = _packed_buffers(desc, plan, qkv, O, lse)
+    _check(lib().cephalo_op_attention_packed_fwd(ctypes.byref(desc), plan, qkv, O, lse, _stream(stream)))
+
+
+def cephalo_op_attention_packed_bwd_workspace(desc):
+    size = int(lib().cephalo_op_attention_packed_bwd_workspace(ctypes.byref(desc)))
+    if size == 0:
+        raise CephaloError(cephalo_last_error())
+    return size
+
+
+def cephalo_op_attention_packed_bwd(desc, plan, qkv, O, dO, lse, dqkv, workspace, stream=None):
+    plan, of_qkv, of_o, qkv, O, lse = _packed_buffers(desc, plan, qkv, O, lse)
+    _check(lib().cephalo_op_attention_packed_bwd(ctypes.byref(desc), plan, qkv, O, _buffer("dO", dO, desc.dtype, of_o), lse, _buffer("dqkv", dqkv, desc.dtype, of_qkv),
+                                                 _ptr(workspace), _nbytes(workspace), _stream(stream)))
+
+
+def cephalo_op_rotary_axes(dtype, src, src_pitch, dst, dst_pitch, positions, rows, axis_dims, heads, head_dim, base=10000.0, inverse=False, stream=None):
+    """axis_dims: the columns of a head that each axis turns (host); positions: int32 [rows, axes]."""
+    last, width = max(rows - 1, 0), heads * head_dim if rows > 0 else 0
+    _check(lib().cephalo_op_rotary_axes(dtype, _buffer("src", src, dtype, last * src_pitch + width), src_pitch, _buffer("dst", dst, dtype, last * dst_pitch + width),
+                                        dst_pitch, _buffer("positions", positions, torch.int32, rows * len(axis_dims)), rows, len(axis_dims), _ints(axis_dims), heads,
+                                        head_dim, base, int(inverse), _stream(stream)))
+
+
+def cephalo_op_dropout_add(dtype, branch, resid, out, n, p, seed, first=0, counter=None, stream=None):
+    """counter: None, or an int64 device tensor whose value is added to `first` when the kernel runs."""
+    counter = None if counter is None else _buffer("counter", counter, torch.int64, 1)
+    _check(lib().cephalo_op_dropout_add(dtype, _buffer("branch", branch, dtype, n), _buffer("resid", resid, torch.float32, n), _buffer("out", out, torch.float32, n),
+                                        n, p, seed, first, counter, _stream(stream)))
+
+
+def cephalo_op_dropout_bwd(dtype, dy, dbranch, n, p, seed, first=0, counter=None, stream=None):
+    counter = None if counter is None else _buffer("counter", counter, torch.int64, 1)
+    _check(lib().cephalo_op_dropout_bwd(dtype, _buffer("dy", dy, torch.float32, n), _buffer("dbranch", dbranch, dtype, n), n, p, seed, first, counter, _stream(stream)))
 
 
 # Names of the 12 tensors of a layer in flat-layout order (see include/cephalo.h).

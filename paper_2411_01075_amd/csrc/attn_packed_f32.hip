@@ -1,0 +1,216 @@
+// fp32 attention over packed samples with grouped heads, forward and backward: the formulas and the blocks' shares of attn_packed.hip on the fp32 matrix
+// products of attn_f32.hip.  A block owns 16 rows, an eighth of an entry of the work list, and its four wavefronts take every fourth block of 16 keys
+// (queries) straight from memory; their results are merged in wavefront order.  Rows past a sample's end are read as zeros.
+#include "attn_f32_tile.h"
+#include "packed.h"
+
+namespace cephalo {
+namespace {
+
+// block l: an eighth of an entry (the eighths of an entry follow one another, the longest work first) and a head
+__device__ __forceinline__ bool packed_sixteenth(const PackedArgs& p, const PackedOrder& order, bool backwards, PackedTile* e, int* unit, int* row0) {
+  const int l = blockIdx.x, per = order.by_xcd ? 8 * ((order.units + 7) >> 3) : order.units;      // blocks of an entry in the order without eighths
+  const int entry = l / (8 * per), rest = l % (8 * per), eighth = rest / per;
+  if (!packed_block(p, order, entry * per + rest % per, e, unit)) return false;
+  const int tile = backwards ? (e->rows + kPackedTile - 1) / kPackedTile - 1 - e->tile : e->tile;
+  *row0 = tile * kPackedTile + 16 * (backwards ? eighth : 7 - eighth);
+  return *row0 < e->rows;
+}
+
+template <int P, bool VEC>
+__global__ void __launch_bounds__(64 * kWaves)
+packed_f32_fwd_kernel(PackedArgs p, PackedOrder order, int causal, const float* __restrict__ qkv, float* __restrict__ O, float* __restrict__ lse) {
+  __shared__ f32x4 red[(kWaves - 1) * P * 64];
+  __shared__ float ml[kWaves][2][16];
+  PackedTile e;
+  int a, q0;
+  if (!packed_sixteenth(p, order, false, &e, &a, &q0)) return;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4;
+  const int S = e.rows, d = p.d, q = q0 + (lane & 15);
+  const float* base = qkv + (int64_t)e.first * p.ld;
+  const float* K = base + (int64_t)(p.heads + a / p.group) * d;
+  const float* V = K + (int64_t)p.kv_heads * d;
+  f32x4 qf[P], o[P];
+  load_rows<P, VEC>(base + a * d, p.ld, q0, S, d, qf);
+#pragma unroll
+  for (int i = 0; i < P; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+  float m = -INFINITY, l = 0.f;
+  const int end = causal ? min(S, q0 + 16) : S;
+  for (int t0 = wave * 16; t0 < end; t0 += 16 * kWaves) {
+    f32x4 kf[P], vf[P];
+    load_rows<P, VEC>(K, p.ld, t0, S, d, kf);
+    load_cols<P>(V, p.ld, t0, S, d, vf);
+    f32x4 s = dot_rows<P>(kf, qf);                         // scores of keys t0 + 4 g + i with query q
+    float mx = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int t = t0 + 4 * g + i;
+      s[i] = (t < S && (!causal || t <= q)) ? s[i] * p.scale : -INFINITY;
+      mx = fmaxf(mx, s[i]);
+    }
+    const float m_new = fmaxf(m, groups_max(mx));          // (this wavefront's maximum of the column)
+    const float shift = m_new == -INFINITY ? 0.f : m_new;
+    const float alpha = expf(m - shift);
+    f32x4 w;
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { w[i] = expf(s[i] - shift); sum += w[i]; }
+    l = l * alpha + sum;
+    m = m_new;
+#pragma unroll
+    for (int i = 0; i < P; ++i) o[i] *= alpha;
+    if (causal && t0 == q0) add_weighted_diagonal<P>(o, vf, w, V, p.ld, t0, S, d, [&](int r) { return t0 + r > q; });
+    else add_weighted<P>(o, vf, w);
+  }
+  l = groups_sum(l);
+  if (g == 0) { ml[wave][0][lane] = m; ml[wave][1][lane] = l; }
+  __syncthreads();
+  float mx = -INFINITY, sum = 0.f;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) mx = fmaxf(mx, ml[w][0][lane & 15]);
+  const float shift = mx == -INFINITY ? 0.f : mx;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) sum += ml[w][1][lane & 15] * expf(ml[w][0][lane & 15] - shift);
+  const float mine = expf(m - shift);
+#pragma unroll
+  for (int i = 0; i < P; ++i) o[i] *= mine;
+  merge_sums<P>(o, red);
+  if (wave == 0) {
+    store_columns<P>(O + (int64_t)e.first * p.ldo + a * d, p.ldo, q, S, d, o, 1.0f / sum);
+    if (g == 0 && q < S) lse[(int64_t)a * p.tokens + e.first + q] = mx + logf(sum);
+  }
+}
+
+template <int P, bool VEC>
+__global__ void __launch_bounds__(64 * kWaves)
+packed_f32_dq_kernel(PackedArgs p, PackedOrder order, int causal, const float* __restrict__ qkv, const float* __restrict__ O, const float* __restrict__ dO,
+                     const float* __restrict__ lse, float* __restrict__ dvec, float* __restrict__ dqkv) {
+  __shared__ f32x4 red[(kWaves - 1) * P * 64];
+  PackedTile e;
+  int a, q0;
+  if (!packed_sixteenth(p, order, false, &e, &a, &q0)) return;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4;
+  const int S = e.rows, d = p.d, q = q0 + (lane & 15);
+  const float* base = qkv + (int64_t)e.first * p.ld;
+  const float* K = base + (int64_t)(p.heads + a / p.group) * d;
+  const float* V = K + (int64_t)p.kv_heads * d;
+  const int64_t orow = (int64_t)e.first * p.ldo + a * d, stat = (int64_t)a * p.tokens + e.first;
+  f32x4 qf[P], dof[P], dq[P];
+  load_rows<P, VEC>(base + a * d, p.ld, q0, S, d, qf);
+  load_rows<P, VEC>(dO + orow, p.ldo, q0, S, d, dof);
+  const float dv = row_dot<P, VEC>(O + orow, p.ldo, q0, S, d, dof);
+  if (wave == 0 && g == 0 && q < S) dvec[stat + q] = dv;
+  const float l = lse[stat + min(q, S - 1)];
+#pragma unroll
+  for (int i = 0; i < P; ++i) dq[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const int end = causal ? min(S, q0 + 16) : S;
+  for (int t0 = wave * 16; t0 < end; t0 += 16 * kWaves) {
+    f32x4 kf[P], vf[P], kc[P];
+    load_rows<P, VEC>(K, p.ld, t0, S, d, kf);
+    load_rows<P, VEC>(V, p.ld, t0, S, d, vf);
+    load_cols<P>(K, p.ld, t0, S, d, kc);
+    const f32x4 s = dot_rows<P>(kf, qf), dp = dot_rows<P>(vf, dof);
+    f32x4 dz;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int t = t0 + 4 * g + i;
+      dz[i] = (t < S && (!causal || t <= q)) ? expf(s[i] * p.scale - l) * (dp[i] - dv) : 0.f;
+    }
+    if (causal && t0 == q0) add_weighted_diagonal<P>(dq, kc, dz, K, p.ld, t0, S, d, [&](int r) { return t0 + r > q; });
+    else add_weighted<P>(dq, kc, dz);
+  }
+  merge_sums<P>(dq, red);
+  if (wave == 0) store_columns<P>(dqkv + (int64_t)e.first * p.ld + a * d, p.ld, q, S, d, dq, p.scale);
+}
+
+template <int P, bool VEC>
+__global__ void __launch_bounds__(64 * kWaves)
+packed_f32_dkv_kernel(PackedArgs p, PackedOrder order, int causal, const float* __restrict__ qkv, const float* __restrict__ dO, const float* __restrict__ lse,
+                      const float* __restrict__ dvec, float* __restrict__ dqkv) {
+  __shared__ f32x4 red[(kWaves - 1) * P * 64];
+  PackedTile e;
+  int kv, t0;
+  if (!packed_sixteenth(p, order, causal, &e, &kv, &t0)) return;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4;
+  const int S = e.rows, d = p.d, t = t0 + (lane & 15);
+  const float* base = qkv + (int64_t)e.first * p.ld;
+  const float* K = base + (int64_t)(p.heads + kv) * d;
+  f32x4 kf[P], vf[P], dk[P], dvv[P];
+  load_rows<P, VEC>(K, p.ld, t0, S, d, kf);
+  load_rows<P, VEC>(K + (int64_t)p.kv_heads * d, p.ld, t0, S, d, vf);
+#pragma unroll
+  for (int i = 0; i < P; ++i) { dk[i] = f32x4{0.f, 0.f, 0.f, 0.f}; dvv[i] = f32x4{0.f, 0.f, 0.f, 0.f}; }
+  for (int a = kv * p.group; a < (kv + 1) * p.group; ++a) {
+    const float* Q = base + a * d;
+    const float* D = dO + (int64_t)e.first * p.ldo + a * d;
+    const int64_t stat = (int64_t)a * p.tokens + e.first;
+    for (int q0 = (causal ? t0 : 0) + wave * 16; q0 < S; q0 += 16 * kWaves) {
+      f32x4 qf[P], dof[P], qc[P], doc[P];
+      load_rows<P, VEC>(Q, p.ld, q0, S, d, qf);
+      load_rows<P, VEC>(D, p.ldo, q0, S, d, dof);
+      load_cols<P>(Q, p.ld, q0, S, d, qc);
+      load_cols<P>(D, p.ldo, q0, S, d, doc);
+      f32x4 l, dv;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int q = min(q0 + 4 * g + i, S - 1);
+        l[i] = lse[stat + q];
+        dv[i] = dvec[stat + q];
+      }
+      const f32x4 s = dot_rows<P>(qf, kf), dp = dot_rows<P>(dof, vf);      // rows: queries q0 + 4 g + i, column: key t
+      f32x4 w, dz;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int q = q0 + 4 * g + i;
+        const bool ok = q < S && (!causal || t <= q);
+        w[i] = ok ? expf(s[i] * p.scale - l[i]) : 0.f;
+        dz[i] = ok ? w[i] * (dp[i] - dv[i]) : 0.f;
+      }
+      if (causal && q0 == t0) {
+        add_weighted_diagonal<P>(dvv, doc, w, D, p.ldo, q0, S, d, [&](int r) { return q0 + r < t; });
+        add_weighted_diagonal<P>(dk, qc, dz, Q, p.ld, q0, S, d, [&](int r) { return q0 + r < t; });
+      } else {
+        add_weighted<P>(dvv, doc, w);
+        add_weighted<P>(dk, qc, dz);
+      }
+    }
+  }
+  float* out = dqkv + (int64_t)e.first * p.ld + (int64_t)(p.heads + kv) * d;
+  merge_sums<P>(dvv, red);
+  if (wave == 0) store_columns<P>(out + (int64_t)p.kv_heads * d, p.ld, t, S, d, dvv, 1.0f);
+  merge_sums<P>(dk, red);
+  if (wave == 0) store_columns<P>(out, p.ld, t, S, d, dk, p.scale);
+}
+
+// pieces of 16 dimensions: 2, 4 or 8 (a head in between runs on the next with zeros)
+#define PACKED_F32_FORMS(CALL)                                                                                    \
+  const int pieces = (a.d + 15) / 16;                                                                             \
+  if (vec) { if (pieces <= 2) { CALL(2, true) } else if (pieces <= 4) { CALL(4, true) } else { CALL(8, true) } }  \
+  else { if (pieces <= 2) { CALL(2, false) } else if (pieces <= 4) { CALL(4, false) } else { CALL(8, false) } }
+}  // namespace
+
+int launch_attn_packed_fwd_f32(const PackedArgs& a, int causal, const float* qkv, float* O, float* lse, hipStream_t s) {
+  const bool vec = a.d % 4 == 0 && a.ld % 4 == 0;
+  PackedOrder order;
+  const unsigned grid = 8 * packed_grid(a, a.heads, &order);
+#define CALL(P, V) packed_f32_fwd_kernel<P, V><<<grid, 64 * kWaves, 0, s>>>(a, order, causal, qkv, O, lse);
+  PACKED_F32_FORMS(CALL)
+#undef CALL
+  CEPHALO_CHECK_LAUNCH("attention_packed_fwd");
+  return CEPHALO_OK;
+}
+
+int launch_attn_packed_bwd_f32(const PackedArgs& a, int causal, const float* qkv, const float* O, const float* dO, const float* lse, float* dvec, float* dqkv, hipStream_t s) {
+  const bool vec = a.d % 4 == 0 && a.ld % 4 == 0 && a.ldo % 4 == 0;
+  PackedOrder order, by_keys;
+  const unsigned grid = 8 * packed_grid(a, a.heads, &order), key_grid = 8 * packed_grid(a, a.kv_heads, &by_keys);
+#define CALL(P, V)                                                                                                       \
+  packed_f32_dq_kernel<P, V><<<grid, 64 * kWaves, 0, s>>>(a, order, causal, qkv, O, dO, lse, dvec, dqkv);                \
+  packed_f32_dkv_kernel<P, V><<<key_grid, 64 * kWaves, 0, s>>>(a, by_keys, causal, qkv, dO, lse, dvec, dqkv);
+  PACKED_F32_FORMS(CALL)
+#undef CALL
+  CEPHALO_CHECK_LAUNCH("attention_packed_bwd");
+  return CEPHALO_OK;
+}
+
+}  // namespace cephalo

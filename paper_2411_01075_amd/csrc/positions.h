@@ -1,0 +1,17 @@
+// Rotary positions with several axes.
+#pragma once
+#include "kernels.h"
+
+namespace cephalo {
+
+constexpr int kMaxRotaryPairs = 64, kMaxAxes = 8;
+struct RotaryAxes {
+  int64_t src_pitch, dst_pitch;      // elements
+  int heads, d, axes, pairs;         // pairs: those that are turned
+  double turns[kMaxRotaryPairs];     // revolutions a position, negative for the inverse
+  unsigned char axis[kMaxRotaryPairs];
+};
+// dst[row][head] = src[row][head] turned, all heads of d columns; positions [rows, axes]; dst may be src
+template <typename T> int launch_rotary_axes(const RotaryAxes& r, const T* src, T* dst, const int* positions, int64_t rows, hipStream_t s);
+
+}  // namespace cephalo

@@ -1,0 +1,68 @@
+// Rotary positions with several axes: pair (2i, 2i+1) of a head is turned by position[row][axis of the pair] * base^(-2 i' / width of the axis), i' its place
+// among the axis's pairs.
+//
+// What bounds it is memory: every element is read and written once.  A thread keeps one 16-byte chunk of a head and takes several heads of a row, whose
+// angles are the same: it forms the chunk's sines and cosines once.  An angle is formed in 64 bits as a number of revolutions, reduced to its
+// fraction and only then rounded: in 32 bits a position of 500 000 is a sixteenth of a radian off.
+#include "positions.h"
+
+namespace cephalo {
+namespace {
+
+template <typename T, int HEADS>
+__global__ void __launch_bounds__(256)
+rotary_axes_kernel(RotaryAxes r, const T* __restrict__ src, T* __restrict__ dst, const int* __restrict__ positions, int64_t rows, int chunks, int parts, int rows_per_block) {
+  constexpr int V = Vec<T>::N, PAIRS = V / 2;
+  const int per_row = chunks * parts, in_block = threadIdx.x / per_row, rest = threadIdx.x % per_row;
+  const int64_t row = (int64_t)blockIdx.x * rows_per_block + in_block;
+  if (in_block >= rows_per_block || row >= rows) return;
+  const int part = rest / chunks, c = rest % chunks, pair0 = c * PAIRS;
+  float cosv[PAIRS], sinv[PAIRS];
+#pragma unroll
+  for (int i = 0; i < PAIRS; ++i) {
+    const int pair = min(pair0 + i, r.pairs - 1);
+    const double turns = (double)positions[row * r.axes + r.axis[pair]] * r.turns[pair];
+    sincospif(2.0f * (float)(turns - rint(turns)), &sinv[i], &cosv[i]);
+  }
+  for (int head0 = part; head0 < r.heads; head0 += parts * HEADS) {
+    float x[HEADS][V];
+#pragma unroll
+    for (int k = 0; k < HEADS; ++k) {
+      const int head = min(head0 + k * parts, r.heads - 1);
+      load_vec<T>(src + row * r.src_pitch + head * r.d + c * V, x[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < HEADS; ++k) {
+      const int head = head0 + k * parts;
+#pragma unroll
+      for (int i = 0; i < PAIRS; ++i) {
+        const float e = x[k][2 * i], o = x[k][2 * i + 1];
+        if (pair0 + i < r.pairs) {                        // (columns past the axes' stay as they are)
+          x[k][2 * i] = e * cosv[i] - o * sinv[i];
+          x[k][2 * i + 1] = e * sinv[i] + o * cosv[i];
+        }
+      }
+      if (head < r.heads) store_vec<T>(dst + row * r.dst_pitch + head * r.d + c * V, x[k]);
+    }
+  }
+}
+
+}  // namespace
+
+template <typename T>
+int launch_rotary_axes(const RotaryAxes& r, const T* src, T* dst, const int* positions, int64_t rows, hipStream_t s) {
+  constexpr int HEADS = 4;
+  const int chunks = r.d / Vec<T>::N;
+  int parts = (r.heads + HEADS - 1) / HEADS;
+  if (parts * chunks > 256) parts = 256 / chunks;
+  const int rows_per_block = 256 / (parts * chunks);
+  const int64_t blocks = (rows + rows_per_block - 1) / rows_per_block;
+  if (blocks >= (int64_t)1 << 31) return fail(CEPHALO_EUNSUPPORTED, "rotary_axes: %lld rows", (long long)rows);
+  rotary_axes_kernel<T, HEADS><<<(unsigned)blocks, 256, 0, s>>>(r, src, dst, positions, rows, chunks, parts, rows_per_block);
+  CEPHALO_CHECK_LAUNCH("rotary_axes");
+  return CEPHALO_OK;
+}
+template int launch_rotary_axes<float>(const RotaryAxes&, const float*, float*, const int*, int64_t, hipStream_t);
+template int launch_rotary_axes<bf16>(const RotaryAxes&, const bf16*, bf16*, const int*, int64_t, hipStream_t);
+
+}  // namespace cephalo

@@ -1,0 +1,376 @@
+"""GPU parity of packed attention, rotary axes and dropout against the oracle in 64 bits, at the sizes, strides and values where they can go wrong.
+
+Tolerances count roundings.  bf16: half a step is 2^-8 of a value.  O is rounded once, and each probability once before it is summed, so
+|O - exact| <= 2^-8 (|O| + sum P |V|); likewise a gradient with |dS| or P in the place of P.  What is computed in fp32 before those roundings (a product's d terms, the
+exponential, a difference dP - rowsum(dO O)) is off by at most FP32 = 2^-14 of the magnitudes summed: (d + 4) 2^-24 < 2^-16 for a product, and the exponent's argument,
+below 64 in these inputs, carries 2^-24 * 64 + (d + 4) 2^-24 * 64 / sqrt(d) < 2^-15 into every probability."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2411_01075_amd as C
+from oracle import packed as opacked
+
+pytestmark = pytest.mark.gpu
+
+HALF = {"bf16": 2.0 ** -8, "f32": 2.0 ** -24}
+FP32 = 2.0 ** -14
+TORCH = {"bf16": torch.bfloat16, "f32": torch.float32}
+LIB = {"bf16": C.BF16, "f32": C.F32}
+MARK = 7.0      # in every place that a call may not touch
+
+
+def _starts(lengths, before=0):
+    return [before + int(v) for v in np.concatenate([[0], np.cumsum(lengths)])]
+
+
+class Packed:
+    """Buffers of one call: rows before and behind the samples and columns past the rows hold MARK."""
+
+    def __init__(self, dtype, heads, kv_heads, d, causal, lengths, before=0, behind=0, gap=0, seed=0, scale=0.0, std=1.0):
+        self.dtype, self.heads, self.kv_heads, self.d, self.causal = dtype, heads, kv_heads, d, causal
+        self.starts = _starts(lengths, before)
+        self.rows = self.starts[-1] + behind
+        self.width, self.o_width = (heads + 2 * kv_heads) * d, heads * d
+        self.desc = C.packed_desc(heads, kv_heads, d, causal, LIB[dtype], self.rows, self.width + gap, self.o_width + gap, scale)
+        self.scale = scale or 1 / math.sqrt(d)
+        self.plan = C.cephalo_packed_plan(self.desc, self.starts).cuda()
+        rng = np.random.default_rng(seed)
+        def buffer(width, inner):
+            t = torch.full((self.rows, width + gap), MARK, dtype=TORCH[dtype])
+            t[before:self.starts[-1], :width] = torch.from_numpy(inner).to(TORCH[dtype])
+            return t.cuda()
+        n = self.starts[-1] - before
+        self.qkv = buffer(self.width, std * rng.standard_normal((n, self.width)))
+        self.dO = buffer(self.o_width, rng.standard_normal((n, self.o_width)))
+        self.O = torch.full_like(self.dO, MARK)
+        self.dqkv = torch.full_like(self.qkv, MARK)
+        self.lse = torch.full((heads, self.rows), MARK, device="cuda")
+        self.workspace = torch.full((C.cephalo_op_attention_packed_bwd_workspace(self.desc),), 0xAB, dtype=torch.uint8, device="cuda")
+
+    def forward(self, **kw):
+        C.cephalo_op_attention_packed_fwd(self.desc, self.plan, self.qkv, self.O, self.lse, **kw)
+
+    def backward(self, **kw):
+        C.cephalo_op_attention_packed_bwd(self.desc, self.plan, self.qkv, self.O, self.dO, self.lse, self.dqkv, self.workspace, **kw)
+
+    def host(self, t, width):
+        return t.double().cpu().numpy()[:, :width]
+
+    def untouched(self, t, width):
+        t = t.float().cpu().numpy()
+        return (t[:self.starts[0]] == MARK).all() and (t[self.starts[-1]:] == MARK).all() and (t[:, width:] == MARK).all()
+
+
+def _within(name, got, want, bound):
+    off = np.abs(got - want) - bound
+    assert np.isfinite(got).all(), "%s has non-finite values" % name
+    assert off.max() <= 0, "%s: off by %.3e where %.3e is allowed" % (name, np.abs(got - want).flat[off.argmax()], bound.flat[off.argmax()])
+
+
+def _check(c):
+    half = HALF[c.dtype]
+    x = c.host(c.qkv, c.width)
+    inside = slice(c.starts[0], c.starts[-1])
+    c.forward()
+    torch.cuda.synchronize()
+    O, lse, mag = opacked.attention_fwd(x, c.starts, c.heads, c.kv_heads, c.d, c.causal, c.scale)
+    _within("O", c.host(c.O, c.o_width)[inside], O[inside], (half * (np.abs(O) + mag) + FP32 * mag)[inside])
+    got = c.lse.double().cpu().numpy()
+    _within("lse", got[:, inside], lse[:, inside], FP32 * (1 + np.abs(lse[:, inside])))
+    assert (got[:, :inside.start] == MARK).all() and (got[:, inside.stop:] == MARK).all()
+    assert c.untouched(c.O, c.o_width)
+    # the backward as a function of what it is given: the forward's own O and lse
+    c.backward()
+    torch.cuda.synchronize()
+    grad, weighted, parts = opacked.attention_bwd(x, c.host(c.O, c.o_width), c.host(c.dO, c.o_width), got, c.starts, c.heads, c.kv_heads, c.d, c.causal, c.scale)
+    _within("dqkv", c.host(c.dqkv, c.width)[inside], grad[inside], (half * (np.abs(grad) + weighted) + FP32 * parts)[inside])
+    assert c.untouched(c.dqkv, c.width)
+
+
+HEADS = [(4, 4, 64), (4, 2, 64), (5, 1, 64), (8, 1, 128), (12, 4, 128), (3, 3, 104), (6, 2, 32), (2, 2, 8), (4, 1, 40), (2, 1, 72)]
+LENGTHS = [[1], [0, 1, 0, 2], [63, 64, 65], [127, 128, 129, 1], [300, 5, 0, 513], [31, 32, 33, 95, 96, 97, 16, 17]]
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("lengths", LENGTHS, ids=str)
+@pytest.mark.parametrize("heads,kv_heads,d", HEADS)
+def test_bf16_attention(heads, kv_heads, d, lengths, causal):
+    print("packed", heads, kv_heads, d, lengths, causal, flush=True)
+    _check(Packed("bf16", heads, kv_heads, d, causal, lengths, seed=d + len(lengths)))
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("lengths", LENGTHS, ids=str)
+@pytest.mark.parametrize("heads,kv_heads,d", [(4, 2, 64), (3, 3, 24), (2, 1, 100), (5, 1, 7), (4, 4, 128)])
+def test_f32_attention(heads, kv_heads, d, lengths, causal):
+    print("packed f32", heads, kv_heads, d, lengths, causal, flush=True)
+    _check(Packed("f32", heads, kv_heads, d, causal, lengths, seed=d + len(lengths)))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("heads,kv_heads,d", [(4, 2, 64), (4, 1, 128), (2, 2, 40)])
+def test_rows_and_columns_that_belong_to_no_sample_stay_as_they_are(heads, kv_heads, d, causal, dtype):
+    _check(Packed(dtype, heads, kv_heads, d, causal, [130, 0, 70, 1], before=3, behind=61, gap=24))
+
+
+@pytest.mark.parametrize("heads,kv_heads,d", [(4, 2, 64), (4, 1, 128)])
+def test_a_scale_of_the_caller_s_and_sharp_scores(heads, kv_heads, d):
+    """Scores of standard deviation 6: rows where one key takes nearly all, and a maximum that moves from tile to tile."""
+    _check(Packed("bf16", heads, kv_heads, d, True, [333, 100], scale=6 / math.sqrt(d)))
+    _check(Packed("f32", heads, kv_heads, d, False, [333, 100], scale=0.37))
+
+
+def test_long_samples():
+    _check(Packed("bf16", 2, 1, 128, True, [2500, 700]))
+    _check(Packed("bf16", 2, 1, 64, False, [1, 2111]))
+
+
+def test_rows_far_apart_pass_32_bits():
+    """Rows of 2 MiB: the samples lie behind 4 GiB, in the projection and in its gradient."""
+    heads, kv_heads, d, pitch, first, lengths = 4, 2, 64, 1 << 20, 2090, [70, 30]
+    rows = first + 100
+    starts = _starts(lengths, first)
+    desc = C.packed_desc(heads, kv_heads, d, True, C.BF16, rows, pitch)
+    plan = C.cephalo_packed_plan(desc, starts).cuda()
+    small = Packed("bf16", heads, kv_heads, d, True, lengths)
+    small.forward(); small.backward()
+    qkv, dqkv = (torch.empty(rows, pitch, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    qkv[first:, :small.width] = small.qkv
+    O, dO, lse = torch.zeros(rows, heads * d, dtype=torch.bfloat16, device="cuda"), torch.zeros(rows, heads * d, dtype=torch.bfloat16, device="cuda"), torch.zeros(heads, rows, device="cuda")
+    dO[first:] = small.dO
+    workspace = torch.empty(C.cephalo_op_attention_packed_bwd_workspace(desc), dtype=torch.uint8, device="cuda")
+    C.cephalo_op_attention_packed_fwd(desc, plan, qkv, O, lse)
+    C.cephalo_op_attention_packed_bwd(desc, plan, qkv, O, dO, lse, dqkv, workspace)
+    torch.cuda.synchronize()
+    assert torch.equal(O[first:], small.O) and torch.equal(lse[:, first:], small.lse)
+    assert torch.equal(dqkv[first:, :small.width], small.dqkv)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("d", [64, 128])
+def test_no_value_crosses_from_sample_to_sample(d, causal, dtype):
+    """One sample of infinities and not-a-numbers: its neighbours' results keep their bits."""
+    lengths, results = [100, 77, 130], []
+    for bad in (False, True):
+        c = Packed(dtype, 4, 2, d, causal, lengths)
+        if bad:
+            c.qkv[100:177] = float("nan")
+            c.qkv[101:177:3] = float("inf")
+            c.dO[100:177] = float("-inf")
+        c.forward(); c.backward()
+        results.append((c.O, c.lse.t().contiguous(), c.dqkv))
+    torch.cuda.synchronize()
+    for a, b in zip(*results):
+        assert torch.equal(a[:100], b[:100]) and torch.equal(a[177:], b[177:])
+
+
+def test_a_sample_s_results_do_not_depend_on_its_neighbours_or_place():
+    for dtype in ("bf16", "f32"):
+        alone = Packed(dtype, 4, 2, 64, True, [200], seed=3)
+        alone.forward(); alone.backward()
+        among = Packed(dtype, 4, 2, 64, True, [7, 200, 300, 1], seed=4)
+        among.qkv[7:207], among.dO[7:207] = alone.qkv, alone.dO
+        among.forward(); among.backward()
+        torch.cuda.synchronize()
+        assert torch.equal(among.O[7:207], alone.O) and torch.equal(among.dqkv[7:207], alone.dqkv) and torch.equal(among.lse[:, 7:207], alone.lse)
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 64), ("bf16", 128), ("f32", 64)])
+def test_the_same_bits_twice_and_under_a_captured_graph(dtype, d):
+    c = Packed(dtype, 8, 2, d, True, [257, 1, 120])
+    c.forward(); c.backward()
+    torch.cuda.synchronize()
+    first = [t.clone() for t in (c.O, c.lse, c.dqkv)]
+    fresh = Packed(dtype, 8, 2, d, True, [257, 1, 120], seed=9)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        c.forward(); c.backward()
+    inputs = [(c.qkv.clone(), c.dO.clone()), (fresh.qkv.clone(), fresh.dO.clone())]
+    fresh.forward(); fresh.backward()
+    torch.cuda.synchronize()
+    second = [t.clone() for t in (fresh.O, fresh.lse, fresh.dqkv)]
+    for k in (0, 1, 0, 1):
+        c.qkv.copy_(inputs[k][0]); c.dO.copy_(inputs[k][1])
+        for t in (c.O, c.lse, c.dqkv):
+            t.fill_(MARK)
+        c.workspace.fill_(0xCD)
+        graph.replay()
+        torch.cuda.synchronize()
+        for got, want in zip((c.O, c.lse, c.dqkv), (first, second)[k]):
+            assert torch.equal(got, want)
+        float((c.dqkv.float() ** 2).sum())      # the program's own work between the replays
+
+
+def test_on_a_stream_of_its_own():
+    a, b = Packed("bf16", 4, 2, 64, True, [300, 20]), Packed("bf16", 4, 2, 64, True, [300, 20])
+    a.forward(); a.backward()
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    b.forward(stream=s); b.backward(stream=s)
+    s.synchronize(); torch.cuda.synchronize()
+    assert torch.equal(a.O, b.O) and torch.equal(a.dqkv, b.dqkv)
+
+
+def test_a_list_of_other_samples_reaches_no_row_outside_the_buffers():
+    """The list's entries are checked against the rows that the call names: of a longer set's list only what fits is done."""
+    big = Packed("bf16", 4, 2, 64, True, [40, 500])
+    c = Packed("bf16", 4, 2, 64, True, [40, 60])
+    c.desc.tiles = big.desc.tiles
+    c.plan = big.plan
+    c.forward(); c.backward()
+    torch.cuda.synchronize()
+    alone = Packed("bf16", 4, 2, 64, True, [40, 60])
+    alone.forward()
+    torch.cuda.synchronize()
+    assert torch.equal(c.O[:40], alone.O[:40]) and bool((c.O[40:] == MARK).all())
+
+
+# ---- rotary axes ------------------------------------------------------------------------------------------------------------
+
+# An angle's fraction of a turn is rounded to 24 bits (2^-25 of a turn: pi 2^-24), a sine or cosine is off by at most two steps (2^-23): 2^-21 of |even| + |odd| covers
+# both, the products and the sum.
+def _rotary(dtype, heads, d, dims, rows, inverse, gap=0, in_place=False, far=0, base=10000.0, seed=0):
+    rng = np.random.default_rng(seed + rows)
+    positions = rng.integers(0, 3000, (rows, len(dims))) + far
+    x = torch.full((max(rows, 1), heads * d + gap), MARK, dtype=TORCH[dtype])
+    x[:rows, :heads * d] = torch.from_numpy(rng.standard_normal((rows, heads * d))).to(TORCH[dtype])
+    src = x.cuda()
+    dst = src if in_place else torch.full_like(src, MARK)
+    C.cephalo_op_rotary_axes(LIB[dtype], src, heads * d + gap, dst, heads * d + gap, torch.from_numpy(positions.astype(np.int32)).cuda(), rows, dims, heads, d, base, inverse)
+    torch.cuda.synchronize()
+    x = x.double().numpy()[:rows, :heads * d]
+    want = opacked.rotary(x, positions, dims, heads, d, base, inverse)
+    pairs = np.abs(x.reshape(-1, 2)).sum(1)[:, None].repeat(2, 1).reshape(x.shape)
+    _within("rotary", dst.double().cpu().numpy()[:rows, :heads * d], want, HALF[dtype] * np.abs(want) + 2.0 ** -21 * pairs)
+    assert (dst.float().cpu().numpy()[:, heads * d:] == MARK).all()
+    turned = sum(dims)
+    same = lambda t: t.reshape(rows, heads, d)[..., turned:]      # noqa: E731
+    assert np.array_equal(same(dst.double().cpu().numpy()[:rows, :heads * d]), same(x))
+
+
+@pytest.mark.parametrize("inverse", [False, True])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("heads,d,dims", [(4, 64, [64]), (1, 8, [4, 4]), (25, 64, [22, 22, 20]), (40, 128, [32, 48, 48]), (3, 80, [40, 0, 20]), (7, 104, [52, 52]), (300, 32, [16, 16]), (2, 128, [2, 30])])
+@pytest.mark.parametrize("rows", [1, 197])
+def test_rotary_axes(heads, d, dims, rows, dtype, inverse):
+    _rotary(dtype, heads, d, dims, rows, inverse)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rotary_in_place_with_gaps_and_at_far_positions(dtype):
+    _rotary(dtype, 6, 64, [20, 22, 22], 133, False, gap=40, in_place=True)
+    _rotary(dtype, 6, 64, [64], 50, True, far=2 ** 31 - 4000)
+    _rotary(dtype, 6, 64, [32, 32], 50, False, far=-700000, base=500000.0)
+    _rotary(dtype, 3, 64, [64], 20011, False)
+
+
+def test_columns_that_are_not_turned_keep_infinities_to_themselves():
+    x = torch.ones(3, 16, device="cuda")
+    x[:, 8] = float("inf"); x[1, 13] = float("nan")
+    y = torch.empty_like(x)
+    C.cephalo_op_rotary_axes(C.F32, x, 16, y, 16, torch.full((3, 1), 5, dtype=torch.int32, device="cuda"), 3, [8], 1, 16)
+    torch.cuda.synchronize()
+    assert torch.equal(y[:, 8:].nan_to_num(3.0), x[:, 8:].nan_to_num(3.0)) and torch.isfinite(y[:, :8]).all()
+
+
+# ---- dropout ----------------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n", [1, 7, 8, 9, 2047, 2048, 2056, 131 * 257])
+@pytest.mark.parametrize("p", [0.0, 0.1, 0.5, 0.999])
+def test_dropout(dtype, n, p):
+    seed, first = 0x9ABCDEF012345678, 8 * (2 ** 33 + 5)
+    rng = np.random.default_rng(n)
+    branch = torch.from_numpy(rng.standard_normal(n)).to(TORCH[dtype]).cuda()
+    resid, dy = (torch.from_numpy(rng.standard_normal(n).astype(np.float32)).cuda() for _ in range(2))
+    out, dbranch = torch.full((n + 8,), MARK, device="cuda"), torch.full((n + 8,), MARK, dtype=TORCH[dtype], device="cuda")
+    C.cephalo_op_dropout_add(LIB[dtype], branch, resid, out, n, p, seed, first)
+    C.cephalo_op_dropout_bwd(LIB[dtype], dy, dbranch, n, p, seed, first)
+    torch.cuda.synchronize()
+    factor = opacked.dropout_factors(n, p, seed, first)
+    got, back = out.double().cpu().numpy(), dbranch.double().cpu().numpy()
+    b, r, g = (t.double().cpu().numpy() for t in (branch, resid, dy))
+    # the scale, the product and the sum are rounded to 24 bits each, the gradient's product to the branch's type
+    _within("out", got[:n], r + factor * b, 2.0 ** -24 * (np.abs(r + factor * b) + 2 * np.abs(factor * b)) * 1.01)
+    _within("dbranch", back[:n], factor * g, (HALF[dtype] + 2.0 ** -23) * np.abs(factor * g) * 1.01)
+    assert ((got[:n] == r) >= (factor == 0)).all() and (back[:n][factor == 0] == 0).all()
+    assert (got[n:] == MARK).all() and (back[n:] == MARK).all()
+
+
+def test_dropped_elements_may_hold_anything_and_out_may_be_resid():
+    n, seed = 4096, 77
+    factor = torch.from_numpy(opacked.dropout_factors(n, 0.5, seed)).cuda()
+    branch, resid = torch.ones(n, device="cuda"), torch.randn(n, device="cuda")
+    branch[factor == 0] = float("nan")
+    want = resid + (factor > 0) * 2.0
+    C.cephalo_op_dropout_add(C.F32, branch, resid, resid, n, 0.5, seed)
+    torch.cuda.synchronize()
+    assert torch.equal(resid, want)
+
+
+def test_parts_of_a_tensor_drop_what_one_call_drops_and_a_counter_moves_the_words():
+    n, seed = 5000, 5
+    x = torch.randn(n, device="cuda")
+    whole, parts, moved = (torch.empty(n, device="cuda") for _ in range(3))
+    C.cephalo_op_dropout_bwd(C.F32, x, whole, n, 0.3, seed, 800)
+    C.cephalo_op_dropout_bwd(C.F32, x[:1600], parts[:1600], 1600, 0.3, seed, 800)
+    C.cephalo_op_dropout_bwd(C.F32, x[1600:], parts[1600:], n - 1600, 0.3, seed, 2400)
+    counter = torch.tensor([0], device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        C.cephalo_op_dropout_bwd(C.F32, x, moved, n, 0.3, seed, 0, counter)
+    torch.cuda.synchronize()
+    assert torch.equal(whole, parts)
+    for at in (800, 16, 800, 2 ** 40):
+        counter.fill_(at)
+        graph.replay()
+        torch.cuda.synchronize()
+        want = torch.from_numpy(opacked.dropout_factors(n, 0.3, seed, at)).cuda()
+        assert torch.equal(moved != 0, want > 0) and (at != 800 or torch.equal(moved, whole))
+
+
+# ---- together ---------------------------------------------------------------------------------------------------------------
+
+def test_the_attention_half_of_a_layer_forward_and_backward():
+    """qkv -> rotary -> attention -> projection -> dropout -> residual, and all the way back, on packed samples in fp32, against the oracle chained in 64 bits.
+
+    The framework's own fp32 tolerance: 1e-4 of the largest value and, on average, of the average one."""
+    heads, kv_heads, d, lengths, H = 6, 2, 32, [50, 1, 129], 192
+    starts, rows, width, p, seed = _starts(lengths), sum(lengths), (6 + 4) * 32, 0.2, 31
+    dims, rng = [16, 8, 8], np.random.default_rng(0)
+    f32 = lambda *shape: rng.standard_normal(shape).astype(np.float32)      # noqa: E731
+    qkv, W, resid, dy, positions = f32(rows, width), f32(H, heads * d) * 0.1, f32(rows, H), f32(rows, H), rng.integers(0, 40, (rows, 3)).astype(np.int32)
+    g = {k: torch.from_numpy(v).cuda() for k, v in dict(qkv=qkv, W=W, resid=resid, dy=dy, positions=positions).items()}
+    new = lambda *shape: torch.full(shape, MARK, device="cuda")      # noqa: E731
+    desc = C.packed_desc(heads, kv_heads, d, True, C.F32, rows)
+    plan = C.cephalo_packed_plan(desc, starts).cuda()
+    turned, O, lse, branch, out = g["qkv"].clone(), new(rows, heads * d), new(heads, rows), new(rows, H), new(rows, H)
+    turn = lambda t, inverse: C.cephalo_op_rotary_axes(C.F32, t, width, t, width, g["positions"], rows, dims, heads + kv_heads, d, 10000.0, inverse)      # noqa: E731
+    turn(turned, False)
+    C.cephalo_op_attention_packed_fwd(desc, plan, turned, O, lse)
+    C.cephalo_op_gemm(C.F32, O, heads * d, 1, g["W"], heads * d, 1, rows, H, heads * d, C.EPI_NONE, branch)
+    C.cephalo_op_dropout_add(C.F32, branch, g["resid"], out, rows * H, p, seed)
+    dbranch, dO, dqkv = new(rows, H), new(rows, heads * d), new(rows, width)
+    C.cephalo_op_dropout_bwd(C.F32, g["dy"], dbranch, rows * H, p, seed)
+    C.cephalo_op_gemm(C.F32, dbranch, H, 1, g["W"], 1, heads * d, rows, heads * d, H, C.EPI_NONE, dO)
+    workspace = torch.empty(C.cephalo_op_attention_packed_bwd_workspace(desc), dtype=torch.uint8, device="cuda")
+    C.cephalo_op_attention_packed_bwd(desc, plan, turned, O, dO, lse, dqkv, workspace)
+    turn(dqkv, True)
+    torch.cuda.synchronize()
+
+    q64 = qkv.astype(np.float64)
+    n = (heads + kv_heads) * d
+    t64 = np.concatenate([opacked.rotary(q64[:, :n], positions, dims, heads + kv_heads, d), q64[:, n:]], axis=1)
+    O64, lse64, _ = opacked.attention_fwd(t64, starts, heads, kv_heads, d, True)
+    factor = opacked.dropout_factors(rows * H, p, seed).reshape(rows, H)
+    out64 = resid + factor * (O64 @ W.astype(np.float64).T)
+    grad, _, _ = opacked.attention_bwd(t64, O64, (factor * dy) @ W.astype(np.float64), lse64, starts, heads, kv_heads, d, True)
+    grad = np.concatenate([opacked.rotary(grad[:, :n], positions, dims, heads + kv_heads, d, inverse=True), grad[:, n:]], axis=1)
+    for name, got, want in (("out", out, out64), ("dqkv", dqkv, grad)):
+        off = np.abs(got.double().cpu().numpy() - want)
+        assert off.max() <= 1e-4 * np.abs(want).max() and off.mean() <= 1e-4 * np.abs(want).mean(), (name, off.max(), off.mean())
