@@ -354,13 +354,15 @@ typedef struct cephalo_packed_desc {
   float   scale;             /* of the scores; 0: 1/sqrt(head_dim) */
   int64_t tokens;            /* rows of qkv, O, dO and dqkv, columns of lse; below 2^31 */
   int64_t qkv_pitch, o_pitch;/* elements from one row of qkv (dqkv) and of O (dO) to the next; in BF16 mode multiples of 8 */
-  int32_t samples, longest, tiles;   /* written by cephalo_packed_plan */
+  int32_t samples, longest, tiles, key_items, joins, slots;   /* these and plan_bytes: written by cephalo_packed_plan */
+  int64_t plan_bytes;
 } cephalo_packed_desc;
 
 /* The work list of a set of samples, made once for all layers and passes that run on them.  Host work only: starts [samples + 1]
  * (not decreasing, inside [0, tokens]) is host memory, and so is `plan`, at least cephalo_packed_plan_bytes(samples, tokens)
- * bytes; the caller copies its first 16 * desc->tiles bytes to the device, where the calls below take it.  Fills samples, longest and
- * tiles of the desc.  A list depends on `causal` and on the starts alone. */
+ * bytes; the caller copies its first desc->plan_bytes bytes to the device, where the calls below take it.  Fills the desc's last fields.
+ * The list holds how the work is divided (128 queries of a sample at a time; 128 keys and all or some of the queries that see them), so it goes
+ * with the desc that it was made for. */
 size_t cephalo_packed_plan_bytes(int32_t samples, int64_t tokens);
 int cephalo_packed_plan(cephalo_packed_desc* desc, int32_t samples, const int32_t* starts, void* plan, size_t plan_bytes);
 

@@ -63,13 +63,14 @@ class ClusterModel(ctypes.Structure):
 class PackedDesc(ctypes.Structure):
     _fields_ = [("heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("causal", ctypes.c_int32), ("dtype", ctypes.c_int32),
                 ("scale", ctypes.c_float), ("tokens", ctypes.c_int64), ("qkv_pitch", ctypes.c_int64), ("o_pitch", ctypes.c_int64),
-                ("samples", ctypes.c_int32), ("longest", ctypes.c_int32), ("tiles", ctypes.c_int32)]
+                ("samples", ctypes.c_int32), ("longest", ctypes.c_int32), ("tiles", ctypes.c_int32), ("key_items", ctypes.c_int32), ("joins", ctypes.c_int32),
+                ("slots", ctypes.c_int32), ("plan_bytes", ctypes.c_int64)]
 
 
 def packed_desc(heads, kv_heads, head_dim, causal, dtype, tokens, qkv_pitch=None, o_pitch=None, scale=0.0):
     """The pitches default to rows without gaps."""
     return PackedDesc(int(heads), int(kv_heads), int(head_dim), int(causal), int(dtype), float(scale), int(tokens),
-                      int((heads + 2 * kv_heads) * head_dim if qkv_pitch is None else qkv_pitch), int(heads * head_dim if o_pitch is None else o_pitch), 0, 0, 0)
+                      int((heads + 2 * kv_heads) * head_dim if qkv_pitch is None else qkv_pitch), int(heads * head_dim if o_pitch is None else o_pitch))
 
 
 _vp, _i32, _i64, _f32, _sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float, ctypes.c_size_t
@@ -188,8 +189,8 @@ def _pinned_ptr(t):
 
 
 def _stream(stream):
-    if stream is None:
-        stream = torch.cuda.current_stream()
+    if stream is None:      # (the handle itself: making a stream object of it takes 2.5 us, as long as a launch)
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
     return stream.cuda_stream
 
 
@@ -410,35 +411,43 @@ def cephalo_op_attention_bwd(desc, qkv, O, dO, lse, dvec, dqkv, micro_batch, str
                                           _ptr(dqkv), micro_batch, _stream(stream)))
 
 
-def _buffer(what, t, dtype, elements):
-    """The address of a device tensor of at least so many elements of that type (dtype: a torch type, or the library's F32 or BF16)."""
-    want = {F32: torch.float32, BF16: torch.bfloat16}.get(dtype, dtype)
-    if t.dtype != want or t.numel() < elements:
+_TYPES = {F32: torch.float32, BF16: torch.bfloat16, "int32": torch.int32, "int64": torch.int64}
+
+
+def _buffer(what, t, dtype, elements, device):
+    """The address of a tensor on the current device (its index is `device`), of at least so many elements of that type."""
+    want = _TYPES.get(dtype)
+    if want is not None and t.dtype is not want or t.numel() < elements:
         raise CephaloError("%s: expected %d elements of %s, got %d of %s" % (what, elements, want, t.numel(), t.dtype))
-    if t.is_cuda and t.device.index != torch.cuda.current_device():
-        raise CephaloError("%s: on %s, but the current device is %d" % (what, t.device, torch.cuda.current_device()))
-    return _ptr(t)
+    if t.get_device() != device:
+        raise CephaloError("%s: expected a device tensor, on the current device (%d), got one on %s" % (what, device, t.device))
+    if not t.is_contiguous():
+        raise CephaloError("%s: expected a contiguous tensor" % what)
+    return t.data_ptr()
+
+
+def _device():
+    return torch.cuda.current_device() if torch.cuda.is_initialized() else -2      # (a host tensor's index is -1)
 
 
 def cephalo_packed_plan(desc, starts):
     """The work list of the samples (rows starts[i] to starts[i + 1]), an int32 host tensor to copy to the device; fills the desc."""
     starts = [int(v) for v in starts]
     size = int(lib().cephalo_packed_plan_bytes(len(starts) - 1, desc.tokens))
-    plan = torch.zeros(max(size, 16) // 16, 4, dtype=torch.int32)
+    plan = torch.zeros(max(size, 16) // 4, dtype=torch.int32)
     _check(lib().cephalo_packed_plan(ctypes.byref(desc), len(starts) - 1, _ints(starts), plan.data_ptr(), plan.numel() * 4))
-    return plan[:max(desc.tiles, 1)].clone()
+    return plan[:max(desc.plan_bytes // 4, 4)].clone()
 
 
-def _packed_buffers(desc, plan, qkv, O, lse):
-    rows = max(desc.tokens - 1, 0)
-    width = desc.heads * desc.head_dim
+def _packed_buffers(desc, plan, qkv, O, lse, device):
+    rows, width, dtype = max(desc.tokens - 1, 0), desc.heads * desc.head_dim, desc.dtype
     of_qkv, of_o = rows * desc.qkv_pitch + width + 2 * desc.kv_heads * desc.head_dim, rows * desc.o_pitch + width
-    return (_buffer("plan", plan, torch.int32, 4 * desc.tiles), of_qkv, of_o, _buffer("qkv", qkv, desc.dtype, of_qkv), _buffer("O", O, desc.dtype, of_o),
-            _buffer("lse", lse, torch.float32, desc.heads * desc.tokens))
+    return (_buffer("plan", plan, "int32", desc.plan_bytes // 4, device), of_qkv, of_o, _buffer("qkv", qkv, dtype, of_qkv, device), _buffer("O", O, dtype, of_o, device),
+            _buffer("lse", lse, F32, desc.heads * desc.tokens, device))
 
 
 def cephalo_op_attention_packed_fwd(desc, plan, qkv, O, lse, stream=None):
-    plan, _, _, qkv, O, lse = _packed_buffers(desc, plan, qkv, O, lse)
+    plan, _, _, qkv, O, lse = _packed_buffers(desc, plan, qkv, O, lse, _device())
     _check(lib().cephalo_op_attention_packed_fwd(ctypes.byref(desc), plan, qkv, O, lse, _stream(stream)))
 
 
@@ -450,29 +459,34 @@ def cephalo_op_attention_packed_bwd_workspace(desc):
 
 
 def cephalo_op_attention_packed_bwd(desc, plan, qkv, O, dO, lse, dqkv, workspace, stream=None):
-    plan, of_qkv, of_o, qkv, O, lse = _packed_buffers(desc, plan, qkv, O, lse)
-    _check(lib().cephalo_op_attention_packed_bwd(ctypes.byref(desc), plan, qkv, O, _buffer("dO", dO, desc.dtype, of_o), lse, _buffer("dqkv", dqkv, desc.dtype, of_qkv),
-                                                 _ptr(workspace), _nbytes(workspace), _stream(stream)))
+    device = _device()
+    plan, of_qkv, of_o, qkv, O, lse = _packed_buffers(desc, plan, qkv, O, lse, device)
+    dO, dqkv = _buffer("dO", dO, desc.dtype, of_o, device), _buffer("dqkv", dqkv, desc.dtype, of_qkv, device)
+    _check(lib().cephalo_op_attention_packed_bwd(ctypes.byref(desc), plan, qkv, O, dO, lse, dqkv, _buffer("workspace", workspace, None, 0, device), _nbytes(workspace),
+                                                 _stream(stream)))
 
 
 def cephalo_op_rotary_axes(dtype, src, src_pitch, dst, dst_pitch, positions, rows, axis_dims, heads, head_dim, base=10000.0, inverse=False, stream=None):
     """axis_dims: the columns of a head that each axis turns (host); positions: int32 [rows, axes]."""
-    last, width = max(rows - 1, 0), heads * head_dim if rows > 0 else 0
-    _check(lib().cephalo_op_rotary_axes(dtype, _buffer("src", src, dtype, last * src_pitch + width), src_pitch, _buffer("dst", dst, dtype, last * dst_pitch + width),
-                                        dst_pitch, _buffer("positions", positions, torch.int32, rows * len(axis_dims)), rows, len(axis_dims), _ints(axis_dims), heads,
-                                        head_dim, base, int(inverse), _stream(stream)))
+    device, last, width, axes = _device(), max(rows - 1, 0), heads * head_dim if rows > 0 else 0, len(axis_dims)
+    src, dst = _buffer("src", src, dtype, last * src_pitch + width, device), _buffer("dst", dst, dtype, last * dst_pitch + width, device)
+    _check(lib().cephalo_op_rotary_axes(dtype, src, src_pitch, dst, dst_pitch, _buffer("positions", positions, "int32", rows * axes, device), rows, axes, _ints(axis_dims),
+                                        heads, head_dim, base, int(inverse), _stream(stream)))
 
 
 def cephalo_op_dropout_add(dtype, branch, resid, out, n, p, seed, first=0, counter=None, stream=None):
     """counter: None, or an int64 device tensor whose value is added to `first` when the kernel runs."""
-    counter = None if counter is None else _buffer("counter", counter, torch.int64, 1)
-    _check(lib().cephalo_op_dropout_add(dtype, _buffer("branch", branch, dtype, n), _buffer("resid", resid, torch.float32, n), _buffer("out", out, torch.float32, n),
-                                        n, p, seed, first, counter, _stream(stream)))
+    device = _device()
+    counter = None if counter is None else _buffer("counter", counter, "int64", 1, device)
+    branch, resid, out = _buffer("branch", branch, dtype, n, device), _buffer("resid", resid, F32, n, device), _buffer("out", out, F32, n, device)
+    _check(lib().cephalo_op_dropout_add(dtype, branch, resid, out, n, p, seed, first, counter, _stream(stream)))
 
 
 def cephalo_op_dropout_bwd(dtype, dy, dbranch, n, p, seed, first=0, counter=None, stream=None):
-    counter = None if counter is None else _buffer("counter", counter, torch.int64, 1)
-    _check(lib().cephalo_op_dropout_bwd(dtype, _buffer("dy", dy, torch.float32, n), _buffer("dbranch", dbranch, dtype, n), n, p, seed, first, counter, _stream(stream)))
+    device = _device()
+    counter = None if counter is None else _buffer("counter", counter, "int64", 1, device)
+    dy, dbranch = _buffer("dy", dy, F32, n, device), _buffer("dbranch", dbranch, dtype, n, device)
+    _check(lib().cephalo_op_dropout_bwd(dtype, dy, dbranch, n, p, seed, first, counter, _stream(stream)))
 
 
 # Names of the 12 tensors of a layer in flat-layout order (see include/cephalo.h).

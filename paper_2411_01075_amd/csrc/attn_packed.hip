@@ -44,7 +44,7 @@ packed_fwd_kernel(PackedArgs p, PackedOrder order, const bf16* __restrict__ qkv,
   auto Vs = [&](int st) { return smem + st * 2 * TL::ELEMS + TL::ELEMS; };
   PackedTile e;
   int a;
-  if (!packed_block(p, order, blockIdx.x, &e, &a)) return;
+  if (!packed_tile(p, order, blockIdx.x, &e, &a)) return;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, h = lane >> 5;
   const int S = e.rows, d = p.d, g = a / p.group;
   const SampleRows x(qkv, p.ld, e.first, S, (p.heads + 2 * p.kv_heads) * d);
@@ -104,7 +104,7 @@ packed_dq_kernel(PackedArgs p, PackedOrder order, const bf16* __restrict__ qkv, 
   auto Vs = [&](int st) { return smem + st * 2 * TL::ELEMS + TL::ELEMS; };
   PackedTile e;
   int a;
-  if (!packed_block(p, order, blockIdx.x, &e, &a)) return;
+  if (!packed_tile(p, order, blockIdx.x, &e, &a)) return;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, h = lane >> 5;
   const int S = e.rows, d = p.d, g = a / p.group;
   const SampleRows x(qkv, p.ld, e.first, S, (p.heads + 2 * p.kv_heads) * d);
@@ -153,14 +153,63 @@ packed_dq_kernel(PackedArgs p, PackedOrder order, const bf16* __restrict__ qkv, 
   store_transposed<D>(dq, dqkv + (int64_t)e.first * p.ld + a * d, p.ld, q, S, p.scale, d);
 }
 
-// The queries that a block of 128 keys walks: for each of the group's heads the tiles of 64 that see the keys.
+// The queries that a block of 128 keys walks: of each of the group's heads the tiles of 64 that see the keys, from step `begin` of that order on.
 struct QueryWalk {
-  int first, end, group, head, it;                     // tiles [first, end) of each head; the next tile to stage
-  __device__ __forceinline__ bool more() const { return head < group; }
+  int first, end, left, head, it;                      // tiles [first, end) of each head; steps left, the next step's head and tile
+  __device__ __forceinline__ QueryWalk(const KeyItem& e, bool causal, int group) {
+    first = walk_first(causal, e.tile) / TILE;
+    end = (e.rows + TILE - 1) / TILE;
+    const int per = end - first;
+    left = e.end - e.begin;
+    head = uniform(e.begin / per);
+    it = first + e.begin - head * per;
+  }
+  __device__ __forceinline__ bool more() const { return left > 0; }
   __device__ __forceinline__ void step() {
+    --left;
     if (++it == end) { it = first; ++head; }
   }
 };
+static_assert(kWalkRows == TILE, "a step of the walk is a tile");
+
+// 16 values of each block of 32 columns (4 consecutive columns of one key, four times) to a place of the workspace, lanes next to one another
+template <int D>
+__device__ __forceinline__ void store_part(const f32x16 (&acc)[D / 32], float* part, int keys32) {
+  f32x4* to = reinterpret_cast<f32x4*>(part) + (size_t)keys32 * (D / 8) * 64 + (threadIdx.x & 63);
+#pragma unroll
+  for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) to[(dt * 4 + j) * 64] = f32x4{acc[dt][4 * j], acc[dt][4 * j + 1], acc[dt][4 * j + 2], acc[dt][4 * j + 3]};
+}
+// dV and dK of 32 keys: to their rows, or to the item's place
+template <int D>
+__device__ __forceinline__ void store_keys(const PackedArgs& p, const KeyItem& e, int g, int t, int keys32, const f32x16 (&dk)[D / 32], const f32x16 (&dvv)[D / 32], bf16* dqkv) {
+  if (e.slot < 0) {
+    bf16* out = dqkv + (int64_t)e.first * p.ld + (p.heads + g) * p.d;
+    store_transposed<D>(dvv, out + p.kv_heads * p.d, p.ld, t, e.rows, 1.0f, p.d);
+    store_transposed<D>(dk, out, p.ld, t, e.rows, p.scale, p.d);
+  } else {
+    float* part = p.part + ((size_t)e.slot * p.kv_heads + g) * (2 * kPackedTile * D);
+    store_part<D>(dvv, part + kPackedTile * D, keys32);
+    store_part<D>(dk, part, keys32);
+  }
+}
+// The places of a join's pieces added in their order.  A thread has 4 columns of one key.
+template <int D>
+__global__ void __launch_bounds__(256) packed_join_kernel(PackedArgs p, bf16* __restrict__ dqkv) {
+  const KeyItem e = p.joins[blockIdx.y];
+  const int g = blockIdx.z, i = blockIdx.x * 256 + threadIdx.x, lane = i & 63, j = (i >> 6) % (D / 8), keys32 = i / (8 * D) % 4, which = i / (32 * D);
+  const int t = e.tile * kPackedTile + keys32 * 32 + (lane & 31), d0 = 8 * j + 4 * (lane >> 5);
+  if (!rows_fit(p, e.first, e.rows, e.tile) || t >= e.rows || d0 >= p.d || e.slot < 0 || e.slot + e.pieces > p.slots) return;
+  const f32x4* part = reinterpret_cast<const f32x4*>(p.part) + ((size_t)e.slot * p.kv_heads + g) * (kPackedTile * D / 2) + i;
+  f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+  for (int q = 0; q < e.pieces; ++q) sum += part[(size_t)q * p.kv_heads * (kPackedTile * D / 2)];
+  const float mul = which ? 1.0f : p.scale;
+  bf16x4 v;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) v[k] = (bf16)(sum[k] * mul);
+  *reinterpret_cast<bf16x4*>(dqkv + ((int64_t)e.first + t) * p.ld + (p.heads + which * p.kv_heads + g) * p.d + d0) = v;
+}
 
 // ------------------------------------------------------------------------------------ dK, dV, heads of 64 or less
 // Four wavefronts of 32 keys, whose rows stay in registers.
@@ -174,19 +223,16 @@ packed_dkv_narrow_kernel(PackedArgs p, PackedOrder order, const bf16* __restrict
   auto Qs = [&](int st) { return smem + st * 2 * TL::ELEMS; };
   auto dOs = [&](int st) { return smem + st * 2 * TL::ELEMS + TL::ELEMS; };
   LDS_AS float* stats = (LDS_AS float*)(smem + 4 * TL::ELEMS);      // [2 buffers][-lse / scale | -dvec][64]
-  PackedTile e;
+  KeyItem e;
   int g;
-  if (!packed_block(p, order, blockIdx.x, &e, &g)) return;
+  if (!packed_keys(p, order, blockIdx.x, CAUSAL, &e, &g)) return;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, h = lane >> 5;
   const int S = e.rows, d = p.d, a0 = g * p.group;
-  // (the list is ordered by what the queries of a tile see; the keys of its mirror image are seen by as many)
-  const int tt = CAUSAL ? (S + 127) / 128 - 1 - e.tile : e.tile;
   const SampleRows x(qkv, p.ld, e.first, S, (p.heads + 2 * p.kv_heads) * d), y(dO, p.ldo, e.first, S, p.heads * d);
   const float c2 = p.scale * kLog2e, per_scale = -1.0f / p.scale;
-  const int t0 = tt * 128 + wave * 32, t = t0 + (lane & 31);
-  const int first = CAUSAL ? tt * 128 / TILE : 0, ntiles = (S + TILE - 1) / TILE;
+  const int t0 = e.tile * 128 + wave * 32, t = t0 + (lane & 31);
 
-  QueryWalk next = {first, ntiles, p.group, 0, first};
+  QueryWalk next(e, CAUSAL, p.group), now = next;
   int buf = 0;                                         // where the next tile goes
   float rstat = 0.f;                                   // threads 0..63: of lse, 64..127: of dvec
   auto stage_next = [&] {
@@ -221,27 +267,25 @@ packed_dkv_narrow_kernel(PackedArgs p, PackedOrder order, const bf16* __restrict
     for (int i = 0; i < 16; ++i) { dk[dt][i] = 0.f; dvv[dt][i] = 0.f; }
   FragAddr<D> at(smem);
   close();
-  const int mine = t0 >= S ? ntiles : CAUSAL ? max(first, t0 / TILE) : first;
+  // of each head's tiles the wavefront's keys are seen from this one on; it helps to stage the others
+  const int mine = t0 >= S ? now.end : CAUSAL ? max(now.first, t0 / TILE) : now.first;
   int cur = 0;
-  for (int head = 0; head < p.group; ++head) {
-    int it = first;
-    for (; it < mine; ++it) {
+  while (now.more()) {
+    for (; now.more() && now.it < mine; now.step()) {
       stage_next();
       at.flip();
       cur ^= 1;
       close();
     }
-    for (; it < ntiles; ++it) {
+    for (; now.more() && now.it >= mine; now.step()) {
       stage_next();
-      dkv_tile<D, CAUSAL, 64>(at, kf, vf, dk, dvv, stats + cur * 128 + 4 * h, c2, t0, t, it * TILE);
+      dkv_tile<D, CAUSAL, 64>(at, kf, vf, dk, dvv, stats + cur * 128 + 4 * h, c2, t0, t, now.it * TILE);
       at.flip();
       cur ^= 1;
       close();
     }
   }
-  bf16* out = dqkv + (int64_t)e.first * p.ld + (p.heads + g) * d;
-  store_transposed<D>(dvv, out + p.kv_heads * d, p.ld, t, S, 1.0f, d);
-  store_transposed<D>(dk, out, p.ld, t, S, p.scale, d);
+  store_keys<D>(p, e, g, t, wave, dk, dvv, dqkv);
 }
 
 // ------------------------------------------------------------------------------------ dK, dV, heads of 65 to 128
@@ -260,22 +304,20 @@ packed_dkv_kernel(PackedArgs p, PackedOrder order, const bf16* __restrict__ qkv,
   lds_bf16* Ks = smem + 4 * TL::ELEMS;
   lds_bf16* Vs = Ks + TKV::ELEMS;
   LDS_AS float* stats = (LDS_AS float*)(Vs + TKV::ELEMS);   // [2 buffers][lse2 | dvec][64]
-  PackedTile e;
+  KeyItem e;
   int g;
-  if (!packed_block(p, order, blockIdx.x, &e, &g)) return;
+  if (!packed_keys(p, order, blockIdx.x, CAUSAL, &e, &g)) return;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, h = lane >> 5;
   const int kg = wave & 3, qh = wave >> 2;
   const int S = e.rows, d = p.d, a0 = g * p.group;
-  const int tt = CAUSAL ? (S + 127) / 128 - 1 - e.tile : e.tile;
   const SampleRows x(qkv, p.ld, e.first, S, (p.heads + 2 * p.kv_heads) * d), y(dO, p.ldo, e.first, S, p.heads * d);
   const float c2 = p.scale * kLog2e;
-  const int t0 = tt * 128 + kg * 32, t = t0 + (lane & 31);
-  const int first = CAUSAL ? tt * 128 / TILE : 0, ntiles = (S + TILE - 1) / TILE;
+  const int t0 = e.tile * 128 + kg * 32, t = t0 + (lane & 31);
 
   const unsigned k_bytes = (unsigned)((p.heads + g) * d * 2), v_bytes = k_bytes + (unsigned)(p.kv_heads * d * 2);
-  TKV::stage(x.rsrc, k_bytes, x.ld_bytes, tt * 128, Ks, d);
-  TKV::stage(x.rsrc, v_bytes, x.ld_bytes, tt * 128, Vs, d);
-  QueryWalk next = {first, ntiles, p.group, 0, first};
+  TKV::stage(x.rsrc, k_bytes, x.ld_bytes, e.tile * 128, Ks, d);
+  TKV::stage(x.rsrc, v_bytes, x.ld_bytes, e.tile * 128, Vs, d);
+  QueryWalk next(e, CAUSAL, p.group), now = next;
   int buf = 0;
   float rstat = 0.f;
   auto stage_next = [&] {
@@ -307,7 +349,6 @@ packed_dkv_kernel(PackedArgs p, PackedOrder order, const bf16* __restrict__ qkv,
     for (int i = 0; i < 16; ++i) { dk[dt][i] = 0.f; dvv[dt][i] = 0.f; }
   close();
 
-  QueryWalk now = {first, ntiles, p.group, 0, first};
   int cur = 0;
   for (; now.more(); now.step()) {
     stage_next();
@@ -375,24 +416,21 @@ packed_dkv_kernel(PackedArgs p, PackedOrder order, const bf16* __restrict__ qkv,
   }
   __syncthreads();
   if (qh == 0) {
-    bf16* out = dqkv + (int64_t)e.first * p.ld + (p.heads + g) * d;
 #pragma unroll
     for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) dvv[dt][i] += mrg[(NV / 2 + dt * 16 + i) * 64];
-    store_transposed<D>(dvv, out + p.kv_heads * d, p.ld, t, S, 1.0f, d);
-#pragma unroll
-    for (int dt = 0; dt < D / 32; ++dt)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) dk[dt][i] += mrg[(dt * 16 + i) * 64];
-    store_transposed<D>(dk, out, p.ld, t, S, p.scale, d);
+      for (int i = 0; i < 16; ++i) {
+        dvv[dt][i] += mrg[(NV / 2 + dt * 16 + i) * 64];
+        dk[dt][i] += mrg[(dt * 16 + i) * 64];
+      }
+    store_keys<D>(p, e, g, t, kg, dk, dvv, dqkv);
   }
 }
 
 template <int D, bool CAUSAL>
 int fwd_cfg(const PackedArgs& a, const bf16* qkv, bf16* O, float* lse, hipStream_t s) {
   PackedOrder order;
-  const unsigned grid = packed_grid(a, a.heads, &order);
+  const unsigned grid = packed_grid(a.tiles, a.heads, &order);
   constexpr auto kern = packed_fwd_kernel<D, CAUSAL>;
   const size_t lds = 4 * (size_t)Tile<D>::ELEMS * sizeof(bf16);      // two stages of 64 keys and values
   if (const int rc = reserve_lds<kern>("attention_packed", lds); rc != CEPHALO_OK) return rc;
@@ -405,14 +443,14 @@ template <int D, bool CAUSAL>
 int bwd_cfg(const PackedArgs& a, const bf16* qkv, const bf16* O, const bf16* dO, const float* lse, float* dvec, bf16* dqkv, hipStream_t s) {
   PackedOrder order;
   {
-    const unsigned grid = packed_grid(a, a.heads, &order);
+    const unsigned grid = packed_grid(a.tiles, a.heads, &order);
     constexpr auto kern = packed_dq_kernel<D, CAUSAL>;
     const size_t lds = 4 * (size_t)Tile<D>::ELEMS * sizeof(bf16);
     if (const int rc = reserve_lds<kern>("attention_packed", lds); rc != CEPHALO_OK) return rc;
     kern<<<grid, kThreads, lds, s>>>(a, order, qkv, O, dO, lse, dvec, dqkv);
     CEPHALO_CHECK_LAUNCH("attention_packed_dq");
   }
-  const unsigned grid = packed_grid(a, a.kv_heads, &order);
+  const unsigned grid = packed_grid(a.key_items, a.kv_heads, &order);
   if constexpr (D <= 64) {
     constexpr auto kern = packed_dkv_narrow_kernel<D, CAUSAL>;
     const size_t lds = 4 * (size_t)Tile<D>::ELEMS * sizeof(bf16) + 2 * 128 * sizeof(float);
@@ -428,6 +466,10 @@ int bwd_cfg(const PackedArgs& a, const bf16* qkv, const bf16* O, const bf16* dO,
     kern<<<grid, kThreads8, lds, s>>>(a, order, qkv, dO, lse, dvec, dqkv);
   }
   CEPHALO_CHECK_LAUNCH("attention_packed_dkv");
+  if (a.join_items > 0) {
+    packed_join_kernel<D><<<dim3(D / 4, a.join_items, a.kv_heads), 256, 0, s>>>(a, dqkv);
+    CEPHALO_CHECK_LAUNCH("attention_packed_join");
+  }
   return CEPHALO_OK;
 }
 

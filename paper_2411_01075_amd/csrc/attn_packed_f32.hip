@@ -7,13 +7,18 @@
 namespace cephalo {
 namespace {
 
-// block l: an eighth of an entry (the eighths of an entry follow one another, the longest work first) and a head
-__device__ __forceinline__ bool packed_sixteenth(const PackedArgs& p, const PackedOrder& order, bool backwards, PackedTile* e, int* unit, int* row0) {
+// block l: an eighth of an entry (the eighths of an entry follow one another) and a head
+__device__ __forceinline__ int packed_eighth(const PackedOrder& order, int* place) {
   const int l = blockIdx.x, per = order.by_xcd ? 8 * ((order.units + 7) >> 3) : order.units;      // blocks of an entry in the order without eighths
-  const int entry = l / (8 * per), rest = l % (8 * per), eighth = rest / per;
-  if (!packed_block(p, order, entry * per + rest % per, e, unit)) return false;
-  const int tile = backwards ? (e->rows + kPackedTile - 1) / kPackedTile - 1 - e->tile : e->tile;
-  *row0 = tile * kPackedTile + 16 * (backwards ? eighth : 7 - eighth);
+  const int rest = l % (8 * per);
+  *place = l / (8 * per) * per + rest % per;
+  return uniform(rest / per);
+}
+__device__ __forceinline__ bool packed_queries(const PackedArgs& p, const PackedOrder& order, PackedTile* e, int* head, int* row0) {
+  int place;
+  const int eighth = packed_eighth(order, &place);
+  if (!packed_tile(p, order, place, e, head)) return false;
+  *row0 = e->tile * kPackedTile + 16 * (7 - eighth);      // (the longest first)
   return *row0 < e->rows;
 }
 
@@ -24,7 +29,7 @@ packed_f32_fwd_kernel(PackedArgs p, PackedOrder order, int causal, const float* 
   __shared__ float ml[kWaves][2][16];
   PackedTile e;
   int a, q0;
-  if (!packed_sixteenth(p, order, false, &e, &a, &q0)) return;
+  if (!packed_queries(p, order, &e, &a, &q0)) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4;
   const int S = e.rows, d = p.d, q = q0 + (lane & 15);
   const float* base = qkv + (int64_t)e.first * p.ld;
@@ -88,7 +93,7 @@ packed_f32_dq_kernel(PackedArgs p, PackedOrder order, int causal, const float* _
   __shared__ f32x4 red[(kWaves - 1) * P * 64];
   PackedTile e;
   int a, q0;
-  if (!packed_sixteenth(p, order, false, &e, &a, &q0)) return;
+  if (!packed_queries(p, order, &e, &a, &q0)) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4;
   const int S = e.rows, d = p.d, q = q0 + (lane & 15);
   const float* base = qkv + (int64_t)e.first * p.ld;
@@ -128,9 +133,12 @@ __global__ void __launch_bounds__(64 * kWaves)
 packed_f32_dkv_kernel(PackedArgs p, PackedOrder order, int causal, const float* __restrict__ qkv, const float* __restrict__ dO, const float* __restrict__ lse,
                       const float* __restrict__ dvec, float* __restrict__ dqkv) {
   __shared__ f32x4 red[(kWaves - 1) * P * 64];
-  PackedTile e;
-  int kv, t0;
-  if (!packed_sixteenth(p, order, causal, &e, &kv, &t0)) return;
+  KeyItem e;
+  int kv, place;
+  const int eighth = packed_eighth(order, &place);
+  if (!packed_keys(p, order, place, causal, &e, &kv)) return;
+  const int t0 = e.tile * kPackedTile + 16 * eighth;
+  if (t0 >= e.rows) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4;
   const int S = e.rows, d = p.d, t = t0 + (lane & 15);
   const float* base = qkv + (int64_t)e.first * p.ld;
@@ -140,46 +148,69 @@ packed_f32_dkv_kernel(PackedArgs p, PackedOrder order, int causal, const float* 
   load_rows<P, VEC>(K + (int64_t)p.kv_heads * d, p.ld, t0, S, d, vf);
 #pragma unroll
   for (int i = 0; i < P; ++i) { dk[i] = f32x4{0.f, 0.f, 0.f, 0.f}; dvv[i] = f32x4{0.f, 0.f, 0.f, 0.f}; }
-  for (int a = kv * p.group; a < (kv + 1) * p.group; ++a) {
+  const int per = walk_steps(causal, S, e.tile);
+  for (int step = e.begin; step < e.end; ++step) {
+    const int a = kv * p.group + step / per, q0 = walk_first(causal, e.tile) + step % per * kWalkRows + wave * 16;
+    if (q0 >= S || (causal && q0 < t0)) continue;        // (16 rows that all lie before the keys see none of them)
     const float* Q = base + a * d;
     const float* D = dO + (int64_t)e.first * p.ldo + a * d;
     const int64_t stat = (int64_t)a * p.tokens + e.first;
-    for (int q0 = (causal ? t0 : 0) + wave * 16; q0 < S; q0 += 16 * kWaves) {
-      f32x4 qf[P], dof[P], qc[P], doc[P];
-      load_rows<P, VEC>(Q, p.ld, q0, S, d, qf);
-      load_rows<P, VEC>(D, p.ldo, q0, S, d, dof);
-      load_cols<P>(Q, p.ld, q0, S, d, qc);
-      load_cols<P>(D, p.ldo, q0, S, d, doc);
-      f32x4 l, dv;
+    f32x4 qf[P], dof[P], qc[P], doc[P];
+    load_rows<P, VEC>(Q, p.ld, q0, S, d, qf);
+    load_rows<P, VEC>(D, p.ldo, q0, S, d, dof);
+    load_cols<P>(Q, p.ld, q0, S, d, qc);
+    load_cols<P>(D, p.ldo, q0, S, d, doc);
+    f32x4 l, dv;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int q = min(q0 + 4 * g + i, S - 1);
-        l[i] = lse[stat + q];
-        dv[i] = dvec[stat + q];
-      }
-      const f32x4 s = dot_rows<P>(qf, kf), dp = dot_rows<P>(dof, vf);      // rows: queries q0 + 4 g + i, column: key t
-      f32x4 w, dz;
+    for (int i = 0; i < 4; ++i) {
+      const int q = min(q0 + 4 * g + i, S - 1);
+      l[i] = lse[stat + q];
+      dv[i] = dvec[stat + q];
+    }
+    const f32x4 s = dot_rows<P>(qf, kf), dp = dot_rows<P>(dof, vf);      // rows: queries q0 + 4 g + i, column: key t
+    f32x4 w, dz;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int q = q0 + 4 * g + i;
-        const bool ok = q < S && (!causal || t <= q);
-        w[i] = ok ? expf(s[i] * p.scale - l[i]) : 0.f;
-        dz[i] = ok ? w[i] * (dp[i] - dv[i]) : 0.f;
-      }
-      if (causal && q0 == t0) {
-        add_weighted_diagonal<P>(dvv, doc, w, D, p.ldo, q0, S, d, [&](int r) { return q0 + r < t; });
-        add_weighted_diagonal<P>(dk, qc, dz, Q, p.ld, q0, S, d, [&](int r) { return q0 + r < t; });
-      } else {
-        add_weighted<P>(dvv, doc, w);
-        add_weighted<P>(dk, qc, dz);
-      }
+    for (int i = 0; i < 4; ++i) {
+      const int q = q0 + 4 * g + i;
+      const bool ok = q < S && (!causal || t <= q);
+      w[i] = ok ? expf(s[i] * p.scale - l[i]) : 0.f;
+      dz[i] = ok ? w[i] * (dp[i] - dv[i]) : 0.f;
+    }
+    if (causal && q0 == t0) {
+      add_weighted_diagonal<P>(dvv, doc, w, D, p.ldo, q0, S, d, [&](int r) { return q0 + r < t; });
+      add_weighted_diagonal<P>(dk, qc, dz, Q, p.ld, q0, S, d, [&](int r) { return q0 + r < t; });
+    } else {
+      add_weighted<P>(dvv, doc, w);
+      add_weighted<P>(dk, qc, dz);
     }
   }
-  float* out = dqkv + (int64_t)e.first * p.ld + (int64_t)(p.heads + kv) * d;
+  float *to_k = dqkv + (int64_t)e.first * p.ld + (int64_t)(p.heads + kv) * d, *to_v = to_k + (int64_t)p.kv_heads * d;
+  int64_t ld = p.ld;
+  int row = t, rows = S;
+  if (e.slot >= 0) {                                     // a place of the workspace: [dK | dV][128][packed_width]
+    ld = packed_width(d);
+    to_k = p.part + ((size_t)e.slot * p.kv_heads + kv) * (2 * kPackedTile * ld);
+    to_v = to_k + kPackedTile * ld;
+    row = t - e.tile * kPackedTile;
+    rows = S - e.tile * kPackedTile;
+  }
   merge_sums<P>(dvv, red);
-  if (wave == 0) store_columns<P>(out + (int64_t)p.kv_heads * d, p.ld, t, S, d, dvv, 1.0f);
+  if (wave == 0) store_columns<P>(to_v, ld, row, rows, d, dvv, 1.0f);
   merge_sums<P>(dk, red);
-  if (wave == 0) store_columns<P>(out, p.ld, t, S, d, dk, p.scale);
+  if (wave == 0) store_columns<P>(to_k, ld, row, rows, d, dk, e.slot >= 0 ? 1.0f : p.scale);
+}
+
+// The places of a join's pieces added in their order, one value a thread.
+__global__ void __launch_bounds__(256) packed_f32_join_kernel(PackedArgs p, float* __restrict__ dqkv) {
+  const KeyItem e = p.joins[blockIdx.y];
+  const int g = blockIdx.z, width = packed_width(p.d), i = blockIdx.x * 256 + threadIdx.x, c = i % width, row = i / width % kPackedTile, which = i / (kPackedTile * width);
+  const int t = e.tile * kPackedTile + row;
+  if (!rows_fit(p, e.first, e.rows, e.tile) || t >= e.rows || c >= p.d || e.slot < 0 || e.slot + e.pieces > p.slots) return;
+  const size_t place = 2 * (size_t)kPackedTile * width;
+  const float* part = p.part + ((size_t)e.slot * p.kv_heads + g) * place + i;
+  float sum = 0.f;
+  for (int q = 0; q < e.pieces; ++q) sum += part[(size_t)q * p.kv_heads * place];
+  dqkv[((int64_t)e.first + t) * p.ld + (int64_t)(p.heads + which * p.kv_heads + g) * p.d + c] = sum * (which ? 1.0f : p.scale);
 }
 
 // pieces of 16 dimensions: 2, 4 or 8 (a head in between runs on the next with zeros)
@@ -192,7 +223,7 @@ packed_f32_dkv_kernel(PackedArgs p, PackedOrder order, int causal, const float* 
 int launch_attn_packed_fwd_f32(const PackedArgs& a, int causal, const float* qkv, float* O, float* lse, hipStream_t s) {
   const bool vec = a.d % 4 == 0 && a.ld % 4 == 0;
   PackedOrder order;
-  const unsigned grid = 8 * packed_grid(a, a.heads, &order);
+  const unsigned grid = 8 * packed_grid(a.tiles, a.heads, &order);
 #define CALL(P, V) packed_f32_fwd_kernel<P, V><<<grid, 64 * kWaves, 0, s>>>(a, order, causal, qkv, O, lse);
   PACKED_F32_FORMS(CALL)
 #undef CALL
@@ -203,13 +234,17 @@ int launch_attn_packed_fwd_f32(const PackedArgs& a, int causal, const float* qkv
 int launch_attn_packed_bwd_f32(const PackedArgs& a, int causal, const float* qkv, const float* O, const float* dO, const float* lse, float* dvec, float* dqkv, hipStream_t s) {
   const bool vec = a.d % 4 == 0 && a.ld % 4 == 0 && a.ldo % 4 == 0;
   PackedOrder order, by_keys;
-  const unsigned grid = 8 * packed_grid(a, a.heads, &order), key_grid = 8 * packed_grid(a, a.kv_heads, &by_keys);
+  const unsigned grid = 8 * packed_grid(a.tiles, a.heads, &order), key_grid = 8 * packed_grid(a.key_items, a.kv_heads, &by_keys);
 #define CALL(P, V)                                                                                                       \
   packed_f32_dq_kernel<P, V><<<grid, 64 * kWaves, 0, s>>>(a, order, causal, qkv, O, dO, lse, dvec, dqkv);                \
   packed_f32_dkv_kernel<P, V><<<key_grid, 64 * kWaves, 0, s>>>(a, by_keys, causal, qkv, dO, lse, dvec, dqkv);
   PACKED_F32_FORMS(CALL)
 #undef CALL
   CEPHALO_CHECK_LAUNCH("attention_packed_bwd");
+  if (a.join_items > 0) {
+    packed_f32_join_kernel<<<dim3(packed_width(a.d), a.join_items, a.kv_heads), 256, 0, s>>>(a, dqkv);
+    CEPHALO_CHECK_LAUNCH("attention_packed_join");
+  }
   return CEPHALO_OK;
 }
 

@@ -16,7 +16,7 @@ int check_dtype(const char* who, int dtype) {
 }
 int check_packed(const char* who, const cephalo_packed_desc* d) {
   if (!d) return fail(CEPHALO_EINVAL, "%s: null desc", who);
-  if (d->heads <= 0 || d->kv_heads <= 0 || d->heads % d->kv_heads != 0)
+  if (d->heads <= 0 || d->heads > 65535 || d->kv_heads <= 0 || d->heads % d->kv_heads != 0)
     return fail(CEPHALO_EINVAL, "%s: %d query heads over %d key heads", who, d->heads, d->kv_heads);
   if (d->head_dim <= 0) return fail(CEPHALO_EINVAL, "%s: head dim %d must be positive", who, d->head_dim);
   if (d->head_dim > 128) return fail(CEPHALO_EUNSUPPORTED, "%s: head dim %d > 128", who, d->head_dim);
@@ -39,12 +39,20 @@ int check_planned(const char* who, const cephalo_packed_desc* d) {
   if (d->samples <= 0 || d->tiles < 0 || d->longest < 0 || d->longest > d->tokens) return fail(CEPHALO_EINVAL, "%s: cephalo_packed_plan has not filled this desc", who);
   if (d->dtype == CEPHALO_BF16 && ((int64_t)d->longest + kPackedTile) * std::max(d->qkv_pitch, d->o_pitch) * 2 >= kRows)
     return fail(CEPHALO_EUNSUPPORTED, "%s: a sample of %d rows exceeds the 2 GiB a buffer offset reaches", who, d->longest);
-  if (((int64_t)d->heads + 7) * d->tiles * 8 >= kRows) return fail(CEPHALO_EUNSUPPORTED, "%s: %d heads of %d tiles are too many blocks", who, d->heads, d->tiles);
+  if (((int64_t)d->heads + 7) * std::max(d->tiles, d->key_items) * 8 >= kRows) return fail(CEPHALO_EUNSUPPORTED, "%s: %d heads of %d tiles are too many blocks", who, d->heads, d->tiles);
+  if (d->key_items < d->tiles || d->joins < 0 || d->joins > d->tiles || d->slots < 0 || d->slots > d->key_items)
+    return fail(CEPHALO_EINVAL, "%s: cephalo_packed_plan has not filled this desc", who);
   return CEPHALO_OK;
 }
+size_t part_bytes(const cephalo_packed_desc* d) { return (size_t)d->slots * d->kv_heads * packed_part_floats(d->head_dim) * sizeof(float); }
+size_t dvec_bytes(const cephalo_packed_desc* d) { return ((size_t)d->heads * d->tokens * sizeof(float) + 255) / 256 * 256; }
 PackedArgs packed_args(const cephalo_packed_desc* d, const void* plan) {
   PackedArgs a;
   a.plan = static_cast<const PackedTile*>(plan);
+  a.keys = reinterpret_cast<const KeyItem*>(a.plan + d->tiles);
+  a.joins = a.keys + d->key_items;
+  a.key_items = d->key_items; a.join_items = d->joins; a.slots = d->slots;
+  a.part = nullptr;
   a.tokens = d->tokens; a.ld = d->qkv_pitch; a.ldo = d->o_pitch;
   a.tiles = d->tiles; a.heads = d->heads; a.kv_heads = d->kv_heads; a.group = d->heads / d->kv_heads; a.d = d->head_dim;
   a.scale = d->scale > 0.f ? d->scale : 1.0f / std::sqrt((float)d->head_dim);
@@ -57,9 +65,24 @@ bool all_aligned(std::initializer_list<const void*> ptrs) {
 }
 }  // namespace
 
+namespace {
+constexpr int kMostPieces = 1024;      // pieces that a list cuts its keys' walks into, beyond one each
+
+// How many steps of a walk an item takes.  A launch lasts as long as its longest block, and a key tile's walk is as long as the queries that see it times the
+// heads that share it, so few keys and long walks leave the chip idle: walks are cut so that none is longer than an equal share of all steps on the
+// compute units' blocks (256 of eight wavefronts, twice that for heads up to 64; fp32 cuts a tile's keys into eighths first).  A piece pays for its place in the
+// workspace, written and read once more, about as much as two or three steps, hence at least kLeast.
+int steps_an_item(const cephalo_packed_desc* d, int64_t steps) {
+  const bool f32 = d->dtype == CEPHALO_F32;
+  const int64_t blocks = f32 ? 64 : d->head_dim > 64 ? 256 : 512, least = f32 ? 2 : 4;
+  return (int)std::min<int64_t>(std::max((steps * d->kv_heads + blocks - 1) / blocks, least), (int64_t)1 << 30);
+}
+}  // namespace
+
 extern "C" size_t cephalo_packed_plan_bytes(int32_t samples, int64_t tokens) {
   if (samples <= 0 || tokens < 0 || tokens >= kRows) return 0;
-  return ((size_t)samples + (size_t)tokens / kPackedTile) * sizeof(PackedTile);
+  const size_t tiles = (size_t)samples + (size_t)tokens / kPackedTile;
+  return tiles * sizeof(PackedTile) + (2 * tiles + kMostPieces) * sizeof(KeyItem);
 }
 
 extern "C" int cephalo_packed_plan(cephalo_packed_desc* d, int32_t samples, const int32_t* starts, void* plan, size_t plan_bytes) {
@@ -75,17 +98,47 @@ extern "C" int cephalo_packed_plan(cephalo_packed_desc* d, int32_t samples, cons
     longest = std::max(longest, starts[i + 1] - starts[i]);
   }
   PackedTile* list = static_cast<PackedTile*>(plan);
+  const int causal = d->causal, group = d->heads / d->kv_heads;
   int tiles = 0;
+  int64_t steps = 0;
   for (int i = 0; i < samples; ++i) {
     const int rows = starts[i + 1] - starts[i];
-    for (int t = 0; (int64_t)t * kPackedTile < rows; ++t) list[tiles++] = {starts[i], rows, t, 0};
+    for (int t = 0; (int64_t)t * kPackedTile < rows; ++t) {
+      list[tiles++] = {starts[i], rows, t, 0};
+      steps += (int64_t)walk_steps(causal, rows, t) * group;
+    }
   }
-  const bool causal = d->causal != 0;
   std::sort(list, list + tiles, [causal](const PackedTile& a, const PackedTile& b) {
     const int wa = causal ? a.tile : a.rows, wb = causal ? b.tile : b.rows;
     return wa != wb ? wa > wb : a.first != b.first ? a.first < b.first : a.tile < b.tile;
   });
-  d->samples = samples; d->longest = longest; d->tiles = tiles;
+  // the walks, cut; an entry of the list stands for the keys of the same tile
+  const int64_t most = steps_an_item(d, steps);
+  int items = 0, joins = 0, slots = 0, spare = kMostPieces;
+  auto pieces_of = [&](const PackedTile& e) {
+    const int64_t walk = (int64_t)walk_steps(causal, e.rows, e.tile) * group;
+    return walk * 4 > most * 5 ? (int)((walk + most - 1) / most) : 1;
+  };
+  KeyItem* keys = reinterpret_cast<KeyItem*>(list + tiles);
+  for (int i = 0; i < tiles; ++i) {
+    const PackedTile& e = list[i];
+    const int64_t walk = (int64_t)walk_steps(causal, e.rows, e.tile) * group;
+    if (walk > (int64_t)1 << 30) return fail(CEPHALO_EUNSUPPORTED, "packed_plan: %d rows under %d heads of a key head", e.rows, group);
+    const int pieces = std::min(pieces_of(e), spare + 1);
+    spare -= pieces - 1;
+    for (int q = 0; q < pieces; ++q)
+      keys[items++] = {e.first, e.rows, e.tile, (int)(walk * q / pieces), (int)(walk * (q + 1) / pieces), pieces > 1 ? slots + q : -1, pieces, 0};
+    if (pieces > 1) { slots += pieces; ++joins; }
+  }
+  KeyItem* join = keys + items;
+  for (int i = 0, k = 0; i < items; ++i)
+    if (keys[i].pieces > 1 && keys[i].begin == 0) join[k++] = keys[i];
+  std::sort(keys, keys + items, [](const KeyItem& a, const KeyItem& b) {
+    const int wa = a.end - a.begin, wb = b.end - b.begin;
+    return wa != wb ? wa > wb : a.first != b.first ? a.first < b.first : a.tile != b.tile ? a.tile < b.tile : a.begin < b.begin;
+  });
+  d->samples = samples; d->longest = longest; d->tiles = tiles; d->key_items = items; d->joins = joins; d->slots = slots;
+  d->plan_bytes = tiles * (int64_t)sizeof(PackedTile) + ((int64_t)items + joins) * (int64_t)sizeof(KeyItem);
   return CEPHALO_OK;
 }
 
@@ -102,7 +155,7 @@ extern "C" int cephalo_op_attention_packed_fwd(const cephalo_packed_desc* d, con
 
 extern "C" size_t cephalo_op_attention_packed_bwd_workspace(const cephalo_packed_desc* d) {
   if (check_planned("attention_packed_bwd_workspace", d) != CEPHALO_OK) return 0;
-  return (size_t)d->heads * d->tokens * sizeof(float) + 256;
+  return dvec_bytes(d) + part_bytes(d);
 }
 
 extern "C" int cephalo_op_attention_packed_bwd(const cephalo_packed_desc* d, const void* plan, const void* qkv, const void* O, const void* dO,
@@ -113,8 +166,9 @@ extern "C" int cephalo_op_attention_packed_bwd(const cephalo_packed_desc* d, con
   if (workspace_bytes < cephalo_op_attention_packed_bwd_workspace(d))
     return fail(CEPHALO_EWORKSPACE, "attention_packed_bwd: workspace %zu B < %zu B", workspace_bytes, cephalo_op_attention_packed_bwd_workspace(d));
   if (d->tiles == 0) return CEPHALO_OK;
-  const PackedArgs a = packed_args(d, plan);
+  PackedArgs a = packed_args(d, plan);
   float* dvec = static_cast<float*>(workspace);
+  a.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + dvec_bytes(d));
   hipStream_t s = static_cast<hipStream_t>(stream);
   if (d->dtype == CEPHALO_F32)
     return launch_attn_packed_bwd_f32(a, d->causal, static_cast<const float*>(qkv), static_cast<const float*>(O), static_cast<const float*>(dO), lse, dvec, static_cast<float*>(dqkv), s);

@@ -4,47 +4,79 @@
 
 namespace cephalo {
 
-// One entry of the work list that cephalo_packed_plan writes: 128 rows of a sample.
+// The work list that cephalo_packed_plan writes: `tiles` PackedTiles, then `key_items` KeyItems, then `joins` KeyItems.
 constexpr int kPackedTile = 128;
-struct PackedTile { int first, rows, tile, spare; };      // the sample's first row, its rows, which 128 of them
+struct PackedTile { int first, rows, tile, spare; };      // 128 rows of a sample: its first row, its rows, which 128 of them
+// 128 keys of a sample and some of the queries that see them, for dK and dV.  The queries of the heads that share the keys, one head after the other, in
+// steps of kWalkRows rows from the first that sees a key: steps [begin, end).  Where an item has them all it writes the results
+// (slot -1), otherwise its 32-bit sums go to place `slot` of the workspace and the join of the same keys adds the `pieces` places from `slot` on.
+struct KeyItem { int first, rows, tile, begin, end, slot, pieces, spare; };
+constexpr int kWalkRows = 64;
 
 // Samples one behind the other in the rows of qkv [tokens, ld]: heads * d columns of queries, kv_heads * d of keys, kv_heads * d of values.  Query head a
 // reads key head a / group.
 struct PackedArgs {
   const PackedTile* plan;
+  const KeyItem* keys;
+  const KeyItem* joins;
   int64_t tokens, ld, ldo;
-  int tiles, heads, kv_heads, group, d;
+  int tiles, key_items, join_items, slots, heads, kv_heads, group, d;
   float scale;
+  float* part;             // dK and dV sums of the items that have a slot: [slot][kv head][packed_part_floats]
 };
+__host__ __device__ inline int packed_width(int d) { return d <= 32 ? 32 : d <= 64 ? 64 : 128; }      // the tile a head of d columns runs on
+inline size_t packed_part_floats(int d) { return 2 * (size_t)kPackedTile * packed_width(d); }
+
+// Steps of a tile's keys over all the heads that share them, and the first row that sees one.
+__host__ __device__ inline int walk_first(int causal, int tile) { return causal ? tile * kPackedTile : 0; }
+__host__ __device__ inline int walk_steps(int causal, int rows, int tile) { return (rows - walk_first(causal, tile) + kWalkRows - 1) / kWalkRows; }
 
 // Which entry of the list and which of `units` heads a block works on.  The list has the longest work first, so the last blocks are short ones; the
 // heads of an entry follow one another.  Blocks are dealt round-robin to the 8 XCDs, each with an L2 of its own: by_xcd gives each XCD an eighth
 // of the heads, so that the heads that share keys (and the tiles of a head) find them in one L2.  Where an XCD would get half as much again as an
 // equal share (5 heads, 12) the blocks go as they are dealt.
 struct PackedOrder { int units, by_xcd; };
-inline unsigned packed_grid(const PackedArgs& a, int units, PackedOrder* order) {
+inline unsigned packed_grid(int entries, int units, PackedOrder* order) {
   const int64_t per = (units + 7) / 8;
   const bool by_xcd = 2 * 8 * per <= 3 * (int64_t)units;
   *order = {units, by_xcd};
-  return (unsigned)(by_xcd ? 8 * per * a.tiles : (int64_t)units * a.tiles);
+  return (unsigned)(by_xcd ? 8 * per * entries : (int64_t)units * entries);
 }
-__device__ __forceinline__ bool packed_block(const PackedArgs& a, const PackedOrder& o, int l, PackedTile* t, int* unit) {
-  int tile, u;
+__device__ __forceinline__ bool packed_block(const PackedOrder& o, int l, int* entry, int* unit) {
+  int e, u;
+  bool any = true;
   if (o.by_xcd) {
     const int xcd = l & 7, i = l >> 3, per = (o.units + 7) >> 3, at = i % per;
     const int first = xcd * o.units >> 3, count = ((xcd + 1) * o.units >> 3) - first;
-    if (at >= count) return false;
-    tile = i / per; u = first + at;
+    any = at < count;
+    e = i / per; u = first + at;
   } else {
-    tile = l / o.units; u = l % o.units;
+    e = l / o.units; u = l % o.units;
   }
   // (the divisions run on the vector unit; readfirstlane tells the compiler that the results are uniform)
-  tile = __builtin_amdgcn_readfirstlane(tile);
+  *entry = __builtin_amdgcn_readfirstlane(e);
   *unit = __builtin_amdgcn_readfirstlane(u);
-  const PackedTile e = a.plan[tile];
-  *t = {__builtin_amdgcn_readfirstlane(e.first), __builtin_amdgcn_readfirstlane(e.rows), __builtin_amdgcn_readfirstlane(e.tile), 0};
-  // (a list that is not this call's reaches no row outside the buffers)
-  return t->first >= 0 && t->rows > 0 && t->tile >= 0 && (int64_t)t->first + t->rows <= a.tokens && (int64_t)t->tile * kPackedTile < t->rows;
+  return any;
+}
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+// (a list that is not this call's reaches no row outside the buffers)
+__device__ __forceinline__ bool rows_fit(const PackedArgs& a, int first, int rows, int tile) {
+  return first >= 0 && rows > 0 && tile >= 0 && (int64_t)first + rows <= a.tokens && (int64_t)tile * kPackedTile < rows;
+}
+__device__ __forceinline__ bool packed_tile(const PackedArgs& a, const PackedOrder& o, int l, PackedTile* t, int* unit) {
+  int entry;
+  if (!packed_block(o, l, &entry, unit)) return false;
+  const PackedTile e = a.plan[entry];
+  *t = {uniform(e.first), uniform(e.rows), uniform(e.tile), 0};
+  return rows_fit(a, t->first, t->rows, t->tile);
+}
+__device__ __forceinline__ bool packed_keys(const PackedArgs& a, const PackedOrder& o, int l, int causal, KeyItem* t, int* unit) {
+  int entry;
+  if (!packed_block(o, l, &entry, unit)) return false;
+  const KeyItem e = a.keys[entry];
+  *t = {uniform(e.first), uniform(e.rows), uniform(e.tile), uniform(e.begin), uniform(e.end), uniform(e.slot), uniform(e.pieces), 0};
+  return rows_fit(a, t->first, t->rows, t->tile) && t->begin >= 0 && t->begin < t->end && t->slot < a.slots &&
+         t->end <= walk_steps(causal, t->rows, t->tile) * a.group;
 }
 
 int launch_attn_packed_fwd_mfma(const PackedArgs& a, int causal, const bf16* qkv, bf16* O, float* lse, hipStream_t s);

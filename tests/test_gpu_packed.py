@@ -124,6 +124,15 @@ def test_a_scale_of_the_caller_s_and_sharp_scores(heads, kv_heads, d):
     _check(Packed("f32", heads, kv_heads, d, False, [333, 100], scale=0.37))
 
 
+@pytest.mark.parametrize("dtype,heads,kv_heads,d", [("bf16", 16, 1, 128), ("bf16", 16, 1, 64), ("bf16", 10, 2, 24), ("f32", 8, 1, 64), ("f32", 6, 1, 50)])
+@pytest.mark.parametrize("causal", [True, False])
+def test_walks_in_pieces(dtype, heads, kv_heads, d, causal):
+    """Few keys under many heads: their queries are cut into pieces whose sums are joined."""
+    c = Packed(dtype, heads, kv_heads, d, causal, [700, 3, 260], gap=8)
+    assert c.desc.joins > 0
+    _check(c)
+
+
 def test_long_samples():
     _check(Packed("bf16", 2, 1, 128, True, [2500, 700]))
     _check(Packed("bf16", 2, 1, 64, False, [1, 2111]))
@@ -220,8 +229,10 @@ def test_a_list_of_other_samples_reaches_no_row_outside_the_buffers():
     """The list's entries are checked against the rows that the call names: of a longer set's list only what fits is done."""
     big = Packed("bf16", 4, 2, 64, True, [40, 500])
     c = Packed("bf16", 4, 2, 64, True, [40, 60])
-    c.desc.tiles = big.desc.tiles
-    c.plan = big.plan
+    for field in ("longest", "tiles", "key_items", "joins", "slots", "plan_bytes"):
+        setattr(c.desc, field, getattr(big.desc, field))
+    c.desc.longest, c.plan = 60, big.plan
+    c.workspace = torch.empty(C.cephalo_op_attention_packed_bwd_workspace(c.desc), dtype=torch.uint8, device="cuda")
     c.forward(); c.backward()
     torch.cuda.synchronize()
     alone = Packed("bf16", 4, 2, 64, True, [40, 60])

@@ -90,16 +90,47 @@ def test_the_list_holds_every_row_once_and_the_longest_work_first(starts, causal
     plan = C.cephalo_packed_plan(d, starts).numpy()
     lengths = [b - a for a, b in zip(starts, starts[1:])]
     assert (d.samples, d.longest, d.tiles) == (len(lengths), max(lengths), sum((n + 127) // 128 for n in lengths))
-    seen = np.zeros(1000, dtype=int)
-    for first, rows, tile, _ in plan[:d.tiles]:
-        assert first in starts and rows in lengths
-        seen[first + tile * 128:min(first + rows, first + tile * 128 + 128)] += 1
+    assert d.plan_bytes == 16 * d.tiles + 32 * (d.key_items + d.joins) <= binding.lib().cephalo_packed_plan_bytes(len(lengths), 1000)
+    tiles, keys, joins = np.split(plan[:d.plan_bytes // 4], [4 * d.tiles, 4 * d.tiles + 8 * d.key_items])
     want = np.zeros(1000, dtype=int)
     want[starts[0]:starts[-1]] = 1
+    seen = np.zeros(1000, dtype=int)
+    tiles = tiles.reshape(-1, 4)
+    for first, rows, tile, _ in tiles:
+        assert first in starts and rows in lengths
+        seen[first + tile * 128:min(first + rows, first + tile * 128 + 128)] += 1
     assert np.array_equal(seen, want)
-    work = [tile if causal else rows for _, rows, tile, _ in plan[:d.tiles]]
+    work = [tile if causal else rows for _, rows, tile, _ in tiles]
     assert work == sorted(work, reverse=True)
-    assert d.tiles * 16 <= binding.lib().cephalo_packed_plan_bytes(len(lengths), 1000)
+
+
+@pytest.mark.parametrize("dtype", [C.BF16, C.F32])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("heads,kv_heads,d,starts", [(4, 2, 64, [0, 1]), (16, 1, 128, [0, 700, 700, 701, 1000]), (8, 8, 64, [5, 900]), (2, 1, 32, [0, 2, 100000]), (40, 8, 128, list(range(0, 64000, 37)))])
+def test_the_walks_of_the_keys_cover_the_queries_once(heads, kv_heads, d, starts, causal, dtype):
+    """Every 128 keys: their items' steps follow one another from 0 to the end, and where there are several each has a place of its own that the join adds in order."""
+    desc = C.packed_desc(heads, kv_heads, d, causal, dtype, starts[-1] + 3)
+    plan = C.cephalo_packed_plan(desc, starts).numpy()
+    _, keys, joins = np.split(plan[:desc.plan_bytes // 4], [4 * desc.tiles, 4 * desc.tiles + 8 * desc.key_items])
+    keys, joins = keys.reshape(-1, 8), joins.reshape(-1, 8)
+    assert [int(e - b) for _, _, _, b, e, _, _, _ in keys] == sorted((int(e - b) for _, _, _, b, e, _, _, _ in keys), reverse=True)
+    by_keys = {}
+    for first, rows, tile, begin, end, slot, pieces, _ in keys.tolist():
+        by_keys.setdefault((first, rows, tile), []).append((begin, end, slot, pieces))
+    assert len(by_keys) == desc.tiles and len(joins) == desc.joins
+    joined, used = {(f, r, t): (s, p) for f, r, t, _, _, s, p, _ in joins.tolist()}, set()
+    for (first, rows, tile), items in by_keys.items():
+        items.sort()
+        steps = (rows - (tile * 128 if causal else 0) + 63) // 64 * (heads // kv_heads)
+        assert items[0][0] == 0 and items[-1][1] == steps and all(a[1] == b[0] and a[0] < a[1] for a, b in zip(items, items[1:] + [(steps, 0, 0, 0)]))
+        assert all(i[3] == len(items) for i in items)
+        if len(items) == 1:
+            assert items[0][2] == -1
+        else:
+            slots = [i[2] for i in items]
+            assert joined.pop((first, rows, tile)) == (slots[0], len(items)) and slots == list(range(slots[0], slots[0] + len(items)))
+            used.update(slots)
+    assert not joined and used == set(range(desc.slots))
 
 
 @pytest.mark.parametrize("starts,says", [([0, 5, 4], "ends before it starts"), ([-1, 5], "from row -1"), ([0, 1001], "to 1001"), ([0], "0 samples")])
@@ -206,7 +237,7 @@ def test_the_binding_refuses_tensors_that_are_too_small_or_of_another_type():
     d = _desc(tokens=10)
     plan = C.cephalo_packed_plan(d, [0, 10])
     qkv, O, lse = torch.zeros(10, 512, dtype=torch.bfloat16), torch.zeros(10, 256, dtype=torch.bfloat16), torch.zeros(4, 10)
-    for args in ((plan[:0], qkv, O, lse), (plan.long(), qkv, O, lse), (plan, qkv[:9], O, lse), (plan, qkv.float(), O, lse), (plan, qkv, O[:9], lse), (plan, qkv, O, lse[:3]),
+    for args in ((plan[:3], qkv, O, lse), (plan.long(), qkv, O, lse), (plan, qkv[:9], O, lse), (plan, qkv.float(), O, lse), (plan, qkv, O[:9], lse), (plan, qkv, O, lse[:3]),
                  (plan, qkv, O, lse.double())):
         with pytest.raises(C.CephaloError, match="expected"):
             C.cephalo_op_attention_packed_fwd(d, *args)
