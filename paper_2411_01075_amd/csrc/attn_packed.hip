@@ -16,6 +16,7 @@ namespace {
 
 constexpr int kThreads8 = 512;
 
+
 // one sample's rows of the packed projection, and of O or dO
 struct SampleRows {
   const bf16* base;
@@ -28,129 +29,349 @@ struct SampleRows {
   }
 };
 
-template <int D> constexpr int kFwdWaves = D == 128 ? 2 : 4;
+template <int D> constexpr int kFwdWaves = D == 128 ? 2 : 3;
 template <int D> constexpr int kDqWaves = D == 32 ? 4 : D == 64 ? 3 : 2;
 template <int D> constexpr int kDkvWaves = D == 32 ? 3 : 2;
 
 // ------------------------------------------------------------------------------------ forward
-// Four wavefronts of 32 queries each, key tiles of 64 in two stages.  The queries of a wavefront see the tiles up to `mine`; it helps to stage the others.
-template <int D, bool CAUSAL>
-__global__ void __launch_bounds__(kThreads, kFwdWaves<D>)
+__device__ __forceinline__ float halves_max(float v) {      // of lanes l and l ^ 32
+  const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, v), __builtin_bit_cast(unsigned, v), false, false);
+  return fmaxf(__builtin_bit_cast(float, r[0]), __builtin_bit_cast(float, r[1]));
+}
+// S^T of the 64 keys of the first stage and a wavefront's 32 queries
+template <int D>
+__device__ __forceinline__ void fwd_scores(const FragAddr<D>& at, const bf16x8 (&qf)[D / 16], f32x16 (&s)[2]) {
+  constexpr int NP = D / 16, kAhead = 3;
+  bf16x8 f[kAhead];
+  f32x16 zero;
+#pragma unroll
+  for (int e = 0; e < 16; ++e) zero[e] = 0.f;
+#pragma unroll
+  for (int i = 0; i < kAhead; ++i) f[i] = at.rows(0, i / NP * 32, i % NP);
+  __builtin_amdgcn_sched_barrier(0);
+  static_steps<2 * NP>([&](auto step) {
+    constexpr int i = decltype(step)::value, b = i / NP, j = i % NP;
+    s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[i % kAhead], qf[j], j == 0 ? zero : s[b], 0, 0, 0);
+    if constexpr (i + kAhead < 2 * NP) f[i % kAhead] = at.rows(0, (i + kAhead) / NP * 32, (i + kAhead) % NP);
+    __builtin_amdgcn_sched_barrier(0);
+  });
+}
+__device__ __forceinline__ void hide_scores(f32x16 (&s)[2], int last) {      // key t0 + 32 b + 8 (e / 4) + e % 4 + 4 h is seen up to `last` of that
+#pragma unroll
+  for (int b = 0; b < 2; ++b)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) s[b][e] = b * 32 + 8 * (e >> 2) + (e & 3) <= last ? s[b][e] : -INFINITY;
+}
+// One tile of the forward, its values in stage BUF: its scores are at hand (s, their maximum mx in the log2 domain), and while its exponentials run on the
+// vector unit the matrix core forms the next tile's scores (NEXT: keys in the other stage, into nx; mx becomes their maximum) and then
+// O^T += V^T P^T.  next_hidden, next_last: whether some keys of the next tile are hidden, and hide_scores' argument.
+template <int D, bool NEXT, int BUF>
+__device__ __forceinline__ void fwd_step(const FragAddr<D>& at, const bf16x8 (&qf)[D / 16], f32x16 (&o)[D / 32], f32x16 (&s)[2], f32x16 (&nx)[2], float& mx, float& m_run,
+                                         float& l_run, float c2, bool next_hidden, int next_last) {
+  constexpr int NP = D / 16, DT = D / 32, NA = NEXT ? 2 * NP : 0, N = NA + 2 * NP, kAhead = NEXT ? 3 : 2;
+  auto fetch = [&](int i) -> bf16x8 {
+    if (i < NA) return at.rows(2 * (BUF ^ 1), i / NP * 32, i % NP);
+    const int k = i - NA, j = k % NP;
+    return at.cols(2 * BUF + 1, j % DT, k / NP * 32 + 16 * (j / DT));
+  };
+  bf16x8 f[kAhead], pf[2][2];
+  f32x16 zero;
+#pragma unroll
+  for (int e = 0; e < 16; ++e) zero[e] = 0.f;
+#pragma unroll
+  for (int i = 0; i < kAhead; ++i) f[i] = fetch(i);
+  __builtin_amdgcn_sched_barrier(0);
+  // Running maximum, in the log2 domain.  It is only raised when some row of the wavefront would otherwise see an exponent above 8 (probabilities up to
+  // 2^8 are harmless in fp32 / bf16 and cancel in the final division); raising it costs a pass over the output accumulators, and after the
+  // first tiles it is rarely needed.
+  if (__any(mx > m_run + 8.0f)) {
+    const float m_new = fmaxf(m_run, mx);
+    const float alpha = (m_new == -INFINITY) ? 1.0f : __builtin_amdgcn_exp2f(m_run - m_new);
+    l_run *= alpha;
+    m_run = m_new;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) o[dt][e] *= alpha;
+  }
+  const float neg_m = (m_run == -INFINITY) ? 0.f : -m_run;
+  float psum = 0.f, m_next = -INFINITY;
+  auto prob = [&](int e) {
+    const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e >> 4][e & 15], c2, neg_m));
+    s[e >> 4][e & 15] = p;
+    psum += p;
+    asm volatile("" : "+v"(s[e >> 4][e & 15]), "+v"(psum));      // (here, under a product: the compiler would move it behind the branch below)
+  };
+  if constexpr (!NEXT) {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) prob(e);
+    pf[0][0] = pack8(s[0], 0); pf[0][1] = pack8(s[0], 8);
+  }
+  static_steps<N>([&](auto step) {
+    constexpr int i = decltype(step)::value, k = i - NA;
+    if constexpr (i < NA) nx[i / NP] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[i % kAhead], qf[i % NP], i % NP == 0 ? zero : nx[i / NP], 0, 0, 0);
+    else o[k % NP % DT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[i % kAhead], pf[k / NP][k % NP / DT], o[k % NP % DT], 0, 0, 0);
+    if constexpr (i + kAhead < N) f[i % kAhead] = fetch(i + kAhead);
+    // the exponentials over the products of the next scores and of the first 32 keys
+    if constexpr (NEXT) {
+#pragma unroll
+      for (int e = i * 32 / (3 * NP); e < (i + 1) * 32 / (3 * NP) && e < 32; ++e) prob(e);
+      if constexpr (i == NA - 1) { pf[0][0] = pack8(s[0], 0); pf[0][1] = pack8(s[0], 8); }
+    } else if constexpr (i < NP) {
+#pragma unroll
+      for (int e = 16 + i * 16 / NP; e < 16 + (i + 1) * 16 / NP; ++e) prob(e);
+    }
+    if constexpr (k == NP - 1) {
+      pf[1][0] = pack8(s[1], 0); pf[1][1] = pack8(s[1], 8);
+      if (NEXT && next_hidden) hide_scores(nx, next_last);
+    }
+    if constexpr (NEXT && k >= NP) {
+#pragma unroll
+      for (int e = (k - NP) * 32 / NP; e < (k - NP + 1) * 32 / NP; ++e) m_next = fmaxf(m_next, nx[e >> 4][e & 15]);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  });
+  l_run += psum;
+  if (NEXT) mx = halves_max(m_next) * c2;                // scores enter the exponent as s * c2 (c2 > 0)
+}
+
+// A block has 32 QW queries, 32 a wavefront, and KG groups of wavefronts that take every KG-th tile of the keys, in two stages of their own; the groups'
+// results are merged at the end.  (4, 1) reads the least from memory and LDS; a launch that leaves compute units idle takes fewer queries a
+// block and several groups.
+template <int QW, int KG> struct Split {
+  static constexpr int THREADS = 64 * QW * KG, ROWS = 32 * QW, PARTS = kPackedTile / ROWS;      // blocks to an entry of the list
+  int wave, group, tiles;                              // place in the group, which group, key tiles of the whole block
+  __device__ __forceinline__ explicit Split(int ntiles) : tiles(ntiles) {
+    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    wave = w % QW; group = w / QW;
+  }
+  __device__ __forceinline__ int at(int i) const { return KG * i + group; }                    // the group's i-th tile
+  __device__ __forceinline__ int rounds() const { return (tiles + KG - 1) / KG; }               // of the group with the most
+  __device__ __forceinline__ int upto(int n) const { return max(0, (n - group + KG - 1) / KG); } // how many of the group's tiles are below n
+};
+// the block's entry of the list, head and first query; false: nothing to do
+template <int QW, int KG>
+__device__ __forceinline__ bool packed_queries(const PackedArgs& p, const PackedOrder& order, int block, PackedTile* e, int* head, int* row0) {
+  constexpr int PARTS = Split<QW, KG>::PARTS;
+  if constexpr (PARTS == 1) {
+    if (!packed_tile(p, order, block, e, head)) return false;
+    *row0 = e->tile * kPackedTile;
+    return true;
+  }
+  const int per = order.by_xcd ? 8 * ((order.units + 7) >> 3) : order.units;      // blocks of an entry in the order without parts
+  const int rest = block % (PARTS * per), part = uniform(rest / per);
+  if (!packed_tile(p, order, block / (PARTS * per) * per + rest % per, e, head)) return false;
+  *row0 = e->tile * kPackedTile + (PARTS - 1 - part) * Split<QW, KG>::ROWS;      // (under a mask the last rows have the most keys)
+  return *row0 < e->rows;
+}
+
+// The keys are staged one tile further ahead than the values.  The queries of a wavefront see the group's first `mine` tiles; it helps to stage the others.
+template <int D, bool CAUSAL, int QW, int KG>
+__global__ void __launch_bounds__(64 * QW * KG, (KG == 1 ? kFwdWaves<D> : D == 128 ? 1 : 2))
 packed_fwd_kernel(PackedArgs p, PackedOrder order, const bf16* __restrict__ qkv, bf16* __restrict__ O, float* __restrict__ lse) {
-  typedef Tile<D> TL;
+  const int block = blockIdx.x;
+  typedef Tile<D, TILE, 64 * QW> TL;
   extern __shared__ __attribute__((aligned(16))) char smem_raw[];
-  lds_bf16* smem = (lds_bf16*)smem_raw;
-  auto Ks = [&](int st) { return smem + st * 2 * TL::ELEMS; };
-  auto Vs = [&](int st) { return smem + st * 2 * TL::ELEMS + TL::ELEMS; };
   PackedTile e;
-  int a;
-  if (!packed_tile(p, order, blockIdx.x, &e, &a)) return;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, h = lane >> 5;
+  int a, r0;
+  if (!packed_queries<QW, KG>(p, order, block, &e, &a, &r0)) return;
+  const int lane = threadIdx.x & 63, h = lane >> 5;
   const int S = e.rows, d = p.d, g = a / p.group;
   const SampleRows x(qkv, p.ld, e.first, S, (p.heads + 2 * p.kv_heads) * d);
   const unsigned k_bytes = (unsigned)((p.heads + g) * d * 2), v_bytes = k_bytes + (unsigned)(p.kv_heads * d * 2);
   const float c2 = p.scale * kLog2e;
-  const int q0 = e.tile * 128 + wave * 32, q = q0 + (lane & 31);
-  const int ntiles = ((CAUSAL ? min(S, e.tile * 128 + 128) : S) + TILE - 1) / TILE;
+  const Split<QW, KG> grp(((CAUSAL ? min(S, r0 + 32 * QW) : S) + TILE - 1) / TILE);
+  const int q0 = r0 + grp.wave * 32;
+  lds_bf16* smem = (lds_bf16*)smem_raw + grp.group * 4 * TL::ELEMS;
+  auto Ks = [&](int st) { return smem + st * 2 * TL::ELEMS; };
+  auto Vs = [&](int st) { return smem + st * 2 * TL::ELEMS + TL::ELEMS; };
 
   bf16x8 qf[D / 16];
   load_row_frags<D>(x.base + a * d, p.ld, q0, S, qf, d);
-  auto stage = [&](int kt) {
-    if (kt >= ntiles) return;
-    TL::stage(x.rsrc, k_bytes, x.ld_bytes, kt * TILE, Ks(kt & 1), d);
-    TL::stage(x.rsrc, v_bytes, x.ld_bytes, kt * TILE, Vs(kt & 1), d);
-  };
+  unsigned part[TL::PER_WAVE];
+  TL::stage_lanes(part, x.ld_bytes, d, grp.wave);
+  const unsigned tile_bytes = TILE * x.ld_bytes;
+  auto stage_keys = [&](int i) { if (grp.at(i) < grp.tiles) TL::stage_at(x.rsrc, part, (unsigned)grp.at(i) * tile_bytes + k_bytes, Ks(i & 1), grp.wave); };
+  auto stage_values = [&](int i) { if (grp.at(i) < grp.tiles) TL::stage_at(x.rsrc, part, (unsigned)grp.at(i) * tile_bytes + v_bytes, Vs(i & 1), grp.wave); };
   auto close = [&] {
     __builtin_amdgcn_s_waitcnt(0x0F70);                // vmcnt(0): this wavefront's rows have landed
     __syncthreads();
   };
-  stage(0);
+  stage_keys(0);
+  stage_keys(1);
+  stage_values(0);
   close();
 
   FragAddr<D> at(smem);
-  f32x16 o[D / 32];
+  at.hold();
+  f32x16 o[D / 32], s0[2], s1[2];
 #pragma unroll
   for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[dt][i] = 0.f;
-  float m_run = -INFINITY, l_run = 0.f;
-  const int mine = q0 >= S ? 0 : CAUSAL ? min(ntiles, (q0 + 31) / TILE + 1) : ntiles;
-  int kt = 0;
-  for (; kt < mine; ++kt) {
-    const int t0 = kt * TILE;
-    stage(kt + 1);
-    fwd_tile<D>(at, qf, o, m_run, l_run, c2, (CAUSAL && t0 + 63 > q0) || t0 + 64 > S, (CAUSAL ? min(q, S - 1) : S - 1) - t0 - 4 * h);
-    at.flip();
+  float m_run = -INFINITY, l_run = 0.f, mx = -INFINITY;
+  const int rounds = grp.rounds(), mine = q0 >= S ? 0 : grp.upto(CAUSAL ? min(grp.tiles, (q0 + 31) / TILE + 1) : grp.tiles);
+  const int limit = (CAUSAL ? min(q0 + (lane & 31), S - 1) : S - 1) - 4 * h;      // the last key that the lane's query sees
+  auto hidden = [&](int kt) { return (CAUSAL && kt * TILE + 63 > q0) || kt * TILE + 64 > S; };
+  if (mine > 0) {
+    fwd_scores<D>(at, qf, s0);
+    if (hidden(grp.at(0))) hide_scores(s0, limit - grp.at(0) * TILE);
+#pragma unroll
+    for (int i = 0; i < 32; ++i) mx = fmaxf(mx, s0[i >> 4][i & 15]);
+    mx = halves_max(mx) * c2;
+  }
+  __syncthreads();                                       // (every wavefront has its scores of tile 0: the keys of tile 2 take its place)
+  int i = 0;
+  auto step = [&](auto next, auto buf, f32x16 (&s)[2], f32x16 (&nx)[2]) {
+    stage_keys(i + 2);
+    stage_values(i + 1);
+    const int kt = grp.at(i + 1);
+    fwd_step<D, decltype(next)::value, decltype(buf)::value>(at, qf, o, s, nx, mx, m_run, l_run, c2, hidden(kt), limit - kt * TILE);
+    close();
+    ++i;
+  };
+  const std::true_type more;
+  const std::false_type end;
+  const std::integral_constant<int, 0> even;
+  const std::integral_constant<int, 1> odd;
+  while (i + 2 < mine) {
+    step(more, even, s0, s1);
+    step(more, odd, s1, s0);
+  }
+  if (i + 1 < mine) {
+    step(more, even, s0, s1);
+    step(end, odd, s1, s0);
+  } else if (i < mine) {
+    step(end, even, s0, s1);
+  }
+  for (; i < rounds; ++i) {
+    stage_keys(i + 2);
+    stage_values(i + 1);
     close();
   }
-  for (; kt < ntiles; ++kt) {
-    stage(kt + 1);
-    close();
+  if constexpr (KG > 1) {                                // [value][lane] floats of each wavefront behind the first group's, lanes next to one another
+    constexpr int NV = D / 32 * 16 + 2;
+    LDS_AS float* mrg = (LDS_AS float*)smem_raw + lane;
+    if (grp.group > 0) {
+      LDS_AS float* to = mrg + ((grp.group - 1) * QW + grp.wave) * NV * 64;
+#pragma unroll
+      for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) to[(dt * 16 + i) * 64] = o[dt][i];
+      to[(NV - 2) * 64] = m_run;
+      to[(NV - 1) * 64] = l_run;
+    }
+    __syncthreads();
+    if (grp.group > 0) return;
+#pragma unroll
+    for (int other = 0; other < KG - 1; ++other) {
+      const LDS_AS float* from = mrg + (other * QW + grp.wave) * NV * 64;
+      const float m1 = from[(NV - 2) * 64], m = fmaxf(m_run, m1);
+      const float a0 = m_run == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_run - m), a1 = m1 == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m1 - m);
+#pragma unroll
+      for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[dt][i] = o[dt][i] * a0 + from[(dt * 16 + i) * 64] * a1;
+      l_run = l_run * a0 + from[(NV - 1) * 64] * a1;
+      m_run = m;
+    }
   }
   const float l_tot = l_run + __shfl_xor(l_run, 32, 64);
+  int at_lane = threadIdx.x & 63;
+  asm volatile("" : "+v"(at_lane));                      // (formed again here, not kept through the loop)
+  const int q = q0 + (at_lane & 31);
   store_transposed<D>(o, O + (int64_t)e.first * p.ldo + a * d, p.ldo, q, S, 1.0f / l_tot, d);
-  if (h == 0 && q < S) lse[(int64_t)a * p.tokens + e.first + q] = (m_run + __builtin_amdgcn_logf(l_tot)) * kLn2;
+  if (at_lane < 32 && q < S) lse[(int64_t)a * p.tokens + e.first + q] = (m_run + __builtin_amdgcn_logf(l_tot)) * kLn2;
 }
 
 // ------------------------------------------------------------------------------------ dQ
-template <int D, bool CAUSAL>
-__global__ void __launch_bounds__(kThreads, kDqWaves<D>)
-packed_dq_kernel(PackedArgs p, PackedOrder order, const bf16* __restrict__ qkv, const bf16* __restrict__ O, const bf16* __restrict__ dO,
-                 const float* __restrict__ lse, float* __restrict__ dvec, bf16* __restrict__ dqkv) {
-  typedef Tile<D> TL;
+// dvec: where rowsum(dO O) goes for the dK / dV blocks, or null
+template <int D, bool CAUSAL, int QW, int KG>
+__device__ __forceinline__ void dq_block(const PackedArgs& p, const PackedOrder& order, int block, const bf16* __restrict__ qkv, const bf16* __restrict__ O,
+                                         const bf16* __restrict__ dO, const float* __restrict__ lse, float* __restrict__ dvec, bf16* __restrict__ dqkv) {
+  typedef Tile<D, TILE, 64 * QW> TL;
   extern __shared__ __attribute__((aligned(16))) char smem_raw[];
-  lds_bf16* smem = (lds_bf16*)smem_raw;
-  auto Ks = [&](int st) { return smem + st * 2 * TL::ELEMS; };
-  auto Vs = [&](int st) { return smem + st * 2 * TL::ELEMS + TL::ELEMS; };
   PackedTile e;
-  int a;
-  if (!packed_tile(p, order, blockIdx.x, &e, &a)) return;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, h = lane >> 5;
+  int a, r0;
+  if (!packed_queries<QW, KG>(p, order, block, &e, &a, &r0)) return;
+  const int lane = threadIdx.x & 63, h = lane >> 5;
   const int S = e.rows, d = p.d, g = a / p.group;
   const SampleRows x(qkv, p.ld, e.first, S, (p.heads + 2 * p.kv_heads) * d);
   const unsigned k_bytes = (unsigned)((p.heads + g) * d * 2), v_bytes = k_bytes + (unsigned)(p.kv_heads * d * 2);
   const float c2 = p.scale * kLog2e;
-  const int q0 = e.tile * 128 + wave * 32, q = q0 + (lane & 31);
-  const int ntiles = ((CAUSAL ? min(S, e.tile * 128 + 128) : S) + TILE - 1) / TILE;
+  const Split<QW, KG> grp(((CAUSAL ? min(S, r0 + 32 * QW) : S) + TILE - 1) / TILE);
+  const int q0 = r0 + grp.wave * 32, q = q0 + (lane & 31);
+  lds_bf16* smem = (lds_bf16*)smem_raw + grp.group * 4 * TL::ELEMS;
+  auto Ks = [&](int st) { return smem + st * 2 * TL::ELEMS; };
+  auto Vs = [&](int st) { return smem + st * 2 * TL::ELEMS + TL::ELEMS; };
 
-  bf16x8 qf[D / 16], dof[D / 16];
-  const int64_t orow = (int64_t)e.first * p.ldo + a * d, stat = (int64_t)a * p.tokens + e.first + q;
-  load_row_frags<D>(dO + orow, p.ldo, q0, S, dof, d);
-  const float dv = row_dot<D>(O + orow, p.ldo, q0, S, dof, d);
-  load_row_frags<D>(x.base + a * d, p.ld, q0, S, qf, d);
-  const float lse2 = q < S ? lse[stat] * kLog2e : 0.f;
-  if (h == 0 && q < S) dvec[stat] = dv;
-  f32x16 dq[D / 32];
-#pragma unroll
-  for (int dt = 0; dt < D / 32; ++dt)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) dq[dt][i] = 0.f;
-  auto stage = [&](int kt) {
-    if (kt >= ntiles) return;
-    TL::stage(x.rsrc, k_bytes, x.ld_bytes, kt * TILE, Ks(kt & 1), d);
-    TL::stage(x.rsrc, v_bytes, x.ld_bytes, kt * TILE, Vs(kt & 1), d);
+  unsigned part[TL::PER_WAVE];
+  TL::stage_lanes(part, x.ld_bytes, d, grp.wave);
+  const unsigned tile_bytes = TILE * x.ld_bytes;
+  auto stage = [&](int i) {
+    if (grp.at(i) >= grp.tiles) return;
+    const unsigned rows = (unsigned)grp.at(i) * tile_bytes;
+    TL::stage_at(x.rsrc, part, rows + k_bytes, Ks(i & 1), grp.wave);
+    TL::stage_at(x.rsrc, part, rows + v_bytes, Vs(i & 1), grp.wave);
   };
   auto close = [&] {
     __builtin_amdgcn_s_waitcnt(0x0F70);                // vmcnt(0)
     __syncthreads();
   };
   stage(0);
+  bf16x8 qf[D / 16], dof[D / 16];
+  const int64_t orow = (int64_t)e.first * p.ldo + a * d, stat = (int64_t)a * p.tokens + e.first + q;
+  load_row_frags<D>(dO + orow, p.ldo, q0, S, dof, d);
+  const float dv = row_dot<D>(O + orow, p.ldo, q0, S, dof, d);
+  load_row_frags<D>(x.base + a * d, p.ld, q0, S, qf, d);
+  const float lse2 = q < S ? lse[stat] * kLog2e : 0.f;
+  if (dvec && h == 0 && q < S && grp.group == 0) dvec[stat] = dv;
+  f32x16 dq[D / 32];
+#pragma unroll
+  for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) dq[dt][i] = 0.f;
   close();
   FragAddr<D> at(smem);
-  const int mine = q0 >= S ? 0 : CAUSAL ? min(ntiles, (q0 + 31) / TILE + 1) : ntiles;
-  int kt = 0;
-  for (; kt < mine; ++kt) {
-    const int t0 = kt * TILE;
-    stage(kt + 1);
-    dq_tile<D>(at, qf, dof, dq, c2, lse2, dv, (CAUSAL && t0 + 63 > q0) || t0 + 64 > S, (CAUSAL ? min(q, S - 1) : S - 1) - t0 - 4 * h);
+  const int rounds = grp.rounds(), mine = q0 >= S ? 0 : grp.upto(CAUSAL ? min(grp.tiles, (q0 + 31) / TILE + 1) : grp.tiles);
+  const int limit = (CAUSAL ? min(q, S - 1) : S - 1) - 4 * h;      // the last key that the lane's query sees
+  int i = 0;
+  for (; i < mine; ++i) {
+    const int t0 = grp.at(i) * TILE;
+    stage(i + 1);
+    dq_tile<D>(at, qf, dof, dq, c2, lse2, dv, (CAUSAL && t0 + 63 > q0) || t0 + 64 > S, limit - t0);
     at.flip();
     close();
   }
-  for (; kt < ntiles; ++kt) {
-    stage(kt + 1);
+  for (; i < rounds; ++i) {
+    stage(i + 1);
     close();
   }
+  if constexpr (KG > 1) {
+    LDS_AS float* mrg = (LDS_AS float*)smem_raw + lane;
+    if (grp.group > 0) {
+#pragma unroll
+      for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) mrg[(((grp.group - 1) * QW + grp.wave) * (D / 32 * 16) + dt * 16 + i) * 64] = dq[dt][i];
+    }
+    __syncthreads();
+    if (grp.group > 0) return;
+#pragma unroll
+    for (int other = 0; other < KG - 1; ++other)
+#pragma unroll
+      for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) dq[dt][i] += mrg[((other * QW + grp.wave) * (D / 32 * 16) + dt * 16 + i) * 64];
+  }
   store_transposed<D>(dq, dqkv + (int64_t)e.first * p.ld + a * d, p.ld, q, S, p.scale, d);
+}
+
+template <int D, bool CAUSAL, int QW, int KG>
+__global__ void __launch_bounds__(64 * QW * KG, (KG == 1 ? kDqWaves<D> : D == 128 ? 1 : 2))
+packed_dq_kernel(PackedArgs p, PackedOrder order, const bf16* __restrict__ qkv, const bf16* __restrict__ O, const bf16* __restrict__ dO,
+                 const float* __restrict__ lse, float* __restrict__ dvec, bf16* __restrict__ dqkv) {
+  dq_block<D, CAUSAL, QW, KG>(p, order, blockIdx.x, qkv, O, dO, lse, dvec, dqkv);
 }
 
 // The queries that a block of 128 keys walks: of each of the group's heads the tiles of 64 that see the keys, from step `begin` of that order on.
@@ -171,6 +392,34 @@ struct QueryWalk {
   }
 };
 static_assert(kWalkRows == TILE, "a step of the walk is a tile");
+
+// rowsum(dO O) of a tile of 64 rows: asked for with the tile, formed when it has landed.  THREADS / 64 threads to a row.
+template <int D, int THREADS> struct OwnRows {
+  static constexpr int PER = THREADS / TILE, N = D / PER / 8;                // 16-byte pieces of a thread
+  bf16x8 o[N], g[N];
+  __device__ __forceinline__ void load(const bf16* __restrict__ O, const bf16* __restrict__ dO, const PackedArgs& p, const KeyItem& e, int head, int row0) {
+    const int r = row0 + threadIdx.x / PER, c0 = threadIdx.x % PER * (D / PER);
+    const int64_t at = ((int64_t)e.first + r) * p.ldo + head * p.d + c0;
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      o[k] = g[k] = bf16x8{0, 0, 0, 0, 0, 0, 0, 0};
+      if (r < e.rows && c0 + 8 * k < p.d) {
+        o[k] = *reinterpret_cast<const bf16x8*>(O + at + 8 * k);
+        g[k] = *reinterpret_cast<const bf16x8*>(dO + at + 8 * k);
+      }
+    }
+  }
+  __device__ __forceinline__ void store(LDS_AS float* to, float sign) const {
+    float v = 0.f;
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v = __builtin_fmaf((float)o[k][i], (float)g[k][i], v);
+#pragma unroll
+    for (int s = 1; s < PER; s *= 2) v += __shfl_xor(v, s, 64);
+    if (threadIdx.x % PER == 0) to[threadIdx.x / PER] = sign * v;
+  }
+};
 
 // 16 values of each block of 32 columns (4 consecutive columns of one key, four times) to a place of the workspace, lanes next to one another
 template <int D>
@@ -213,10 +462,10 @@ __global__ void __launch_bounds__(256) packed_join_kernel(PackedArgs p, bf16* __
 
 // ------------------------------------------------------------------------------------ dK, dV, heads of 64 or less
 // Four wavefronts of 32 keys, whose rows stay in registers.
-template <int D, bool CAUSAL>
-__global__ void __launch_bounds__(kThreads, kDkvWaves<D>)
-packed_dkv_narrow_kernel(PackedArgs p, PackedOrder order, const bf16* __restrict__ qkv, const bf16* __restrict__ dO, const float* __restrict__ lse,
-                         const float* __restrict__ dvec, bf16* __restrict__ dqkv) {
+// OWN: rowsum(dO O) is formed here, from O, not read from dvec.
+template <int D, bool CAUSAL, bool OWN>
+__device__ __forceinline__ void dkv_narrow_block(const PackedArgs& p, const PackedOrder& order, int block, const bf16* __restrict__ qkv, const bf16* __restrict__ O,
+                                                 const bf16* __restrict__ dO, const float* __restrict__ lse, const float* __restrict__ dvec, bf16* __restrict__ dqkv) {
   typedef Tile<D> TL;
   extern __shared__ __attribute__((aligned(16))) char smem_raw[];
   lds_bf16* smem = (lds_bf16*)smem_raw;
@@ -225,7 +474,7 @@ packed_dkv_narrow_kernel(PackedArgs p, PackedOrder order, const bf16* __restrict
   LDS_AS float* stats = (LDS_AS float*)(smem + 4 * TL::ELEMS);      // [2 buffers][-lse / scale | -dvec][64]
   KeyItem e;
   int g;
-  if (!packed_keys(p, order, blockIdx.x, CAUSAL, &e, &g)) return;
+  if (!packed_keys(p, order, block, CAUSAL, &e, &g)) return;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, h = lane >> 5;
   const int S = e.rows, d = p.d, a0 = g * p.group;
   const SampleRows x(qkv, p.ld, e.first, S, (p.heads + 2 * p.kv_heads) * d), y(dO, p.ldo, e.first, S, p.heads * d);
@@ -235,6 +484,8 @@ packed_dkv_narrow_kernel(PackedArgs p, PackedOrder order, const bf16* __restrict
   QueryWalk next(e, CAUSAL, p.group), now = next;
   int buf = 0;                                         // where the next tile goes
   float rstat = 0.f;                                   // threads 0..63: of lse, 64..127: of dvec
+  OwnRows<D, kThreads> own;
+  constexpr float kSign = -1.0f;
   auto stage_next = [&] {
     if (!next.more()) return;
     const unsigned col = (unsigned)((a0 + next.head) * d * 2);
@@ -242,14 +493,16 @@ packed_dkv_narrow_kernel(PackedArgs p, PackedOrder order, const bf16* __restrict
     TL::stage(y.rsrc, col, y.ld_bytes, next.it * TILE, dOs(buf), d);
     rstat = 0.f;
     const int r = next.it * TILE + (threadIdx.x & 63);
-    if (threadIdx.x < 128 && r < S) {
+    if (threadIdx.x < (OWN ? 64 : 128) && r < S) {
       const int64_t at = (int64_t)(a0 + next.head) * p.tokens + e.first + r;
       rstat = threadIdx.x < 64 ? lse[at] * per_scale : -dvec[at];
     }
+    if constexpr (OWN) own.load(O, dO, p, e, a0 + next.head, next.it * TILE);
   };
   auto close = [&] {                                   // the tile that was staged becomes the current one
     if (next.more()) {
-      if (threadIdx.x < 128) stats[buf * 128 + threadIdx.x] = rstat;
+      if (threadIdx.x < (OWN ? 64 : 128)) stats[buf * 128 + threadIdx.x] = rstat;
+      if constexpr (OWN) own.store(stats + buf * 128 + 64, kSign);
       next.step();
       buf ^= 1;
     }
@@ -291,10 +544,9 @@ packed_dkv_narrow_kernel(PackedArgs p, PackedOrder order, const bf16* __restrict
 // ------------------------------------------------------------------------------------ dK, dV, heads of 65 to 128
 // Eight wavefronts: wavefront w takes 32 of the 128 keys (w & 3) and of every 64 queries the 32 of half w >> 2.  The keys and values stay in LDS: in
 // registers they would push the accumulators out of the file that the vector unit reads.
-template <int D, bool CAUSAL>
-__global__ void __launch_bounds__(kThreads8, 2)
-packed_dkv_kernel(PackedArgs p, PackedOrder order, const bf16* __restrict__ qkv, const bf16* __restrict__ dO, const float* __restrict__ lse,
-                  const float* __restrict__ dvec, bf16* __restrict__ dqkv) {
+template <int D, bool CAUSAL, bool OWN>
+__device__ __forceinline__ void dkv_wide_block(const PackedArgs& p, const PackedOrder& order, int block, const bf16* __restrict__ qkv, const bf16* __restrict__ O,
+                                               const bf16* __restrict__ dO, const float* __restrict__ lse, const float* __restrict__ dvec, bf16* __restrict__ dqkv) {
   typedef Tile<D, TILE, kThreads8> TL;
   typedef Tile<D, 128, kThreads8> TKV;
   extern __shared__ __attribute__((aligned(16))) char smem_raw[];
@@ -306,7 +558,7 @@ packed_dkv_kernel(PackedArgs p, PackedOrder order, const bf16* __restrict__ qkv,
   LDS_AS float* stats = (LDS_AS float*)(Vs + TKV::ELEMS);   // [2 buffers][lse2 | dvec][64]
   KeyItem e;
   int g;
-  if (!packed_keys(p, order, blockIdx.x, CAUSAL, &e, &g)) return;
+  if (!packed_keys(p, order, block, CAUSAL, &e, &g)) return;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, h = lane >> 5;
   const int kg = wave & 3, qh = wave >> 2;
   const int S = e.rows, d = p.d, a0 = g * p.group;
@@ -320,6 +572,8 @@ packed_dkv_kernel(PackedArgs p, PackedOrder order, const bf16* __restrict__ qkv,
   QueryWalk next(e, CAUSAL, p.group), now = next;
   int buf = 0;
   float rstat = 0.f;
+  OwnRows<D, kThreads8> own;
+  constexpr float kSign = 1.0f;
   auto stage_next = [&] {
     if (!next.more()) return;
     const unsigned col = (unsigned)((a0 + next.head) * d * 2);
@@ -327,14 +581,16 @@ packed_dkv_kernel(PackedArgs p, PackedOrder order, const bf16* __restrict__ qkv,
     TL::stage(y.rsrc, col, y.ld_bytes, next.it * TILE, dOs(buf), d);
     rstat = 0.f;
     const int r = next.it * TILE + (threadIdx.x & 63);
-    if (threadIdx.x < 128 && r < S) {
+    if (threadIdx.x < (OWN ? 64 : 128) && r < S) {
       const int64_t at = (int64_t)(a0 + next.head) * p.tokens + e.first + r;
       rstat = threadIdx.x < 64 ? lse[at] * kLog2e : dvec[at];
     }
+    if constexpr (OWN) own.load(O, dO, p, e, a0 + next.head, next.it * TILE);
   };
   auto close = [&] {
     if (next.more()) {
-      if (threadIdx.x < 128) stats[buf * 128 + threadIdx.x] = rstat;
+      if (threadIdx.x < (OWN ? 64 : 128)) stats[buf * 128 + threadIdx.x] = rstat;
+      if constexpr (OWN) own.store(stats + buf * 128 + 64, kSign);
       next.step();
       buf ^= 1;
     }
@@ -428,49 +684,104 @@ packed_dkv_kernel(PackedArgs p, PackedOrder order, const bf16* __restrict__ qkv,
 }
 
 template <int D, bool CAUSAL>
-int fwd_cfg(const PackedArgs& a, const bf16* qkv, bf16* O, float* lse, hipStream_t s) {
+__global__ void __launch_bounds__(kThreads, kDkvWaves<D>)
+packed_dkv_narrow_kernel(PackedArgs p, PackedOrder order, const bf16* __restrict__ qkv, const bf16* __restrict__ dO, const float* __restrict__ lse,
+                         const float* __restrict__ dvec, bf16* __restrict__ dqkv) {
+  dkv_narrow_block<D, CAUSAL, false>(p, order, blockIdx.x, qkv, nullptr, dO, lse, dvec, dqkv);
+}
+template <int D, bool CAUSAL>
+__global__ void __launch_bounds__(kThreads8, 2)
+packed_dkv_kernel(PackedArgs p, PackedOrder order, const bf16* __restrict__ qkv, const bf16* __restrict__ dO, const float* __restrict__ lse,
+                  const float* __restrict__ dvec, bf16* __restrict__ dqkv) {
+  dkv_wide_block<D, CAUSAL, false>(p, order, blockIdx.x, qkv, nullptr, dO, lse, dvec, dqkv);
+}
+// The whole backward in one launch, where one after the other its two halves would leave compute units idle: the blocks of dK and dV, the longer ones, first.
+// They form rowsum(dO O) themselves.
+template <int D> constexpr int kBothThreads = D <= 64 ? kThreads : kThreads8;
+template <int D, bool CAUSAL>
+__global__ void __launch_bounds__(kBothThreads<D>, 2)
+packed_bwd_kernel(PackedArgs p, PackedOrder by_keys, PackedOrder by_queries, int key_blocks, const bf16* __restrict__ qkv, const bf16* __restrict__ O,
+                  const bf16* __restrict__ dO, const float* __restrict__ lse, bf16* __restrict__ dqkv) {
+  const int block = blockIdx.x;
+  if (block >= key_blocks) dq_block<D, CAUSAL, D <= 64 ? 2 : 4, 2>(p, by_queries, block - key_blocks, qkv, O, dO, lse, nullptr, dqkv);
+  else if constexpr (D <= 64) dkv_narrow_block<D, CAUSAL, true>(p, by_keys, block, qkv, O, dO, lse, nullptr, dqkv);
+  else dkv_wide_block<D, CAUSAL, true>(p, by_keys, block, qkv, O, dO, lse, nullptr, dqkv);
+}
+
+template <int D, bool CAUSAL, int QW, int KG>
+int launch_fwd(const PackedArgs& a, const bf16* qkv, bf16* O, float* lse, hipStream_t s) {
   PackedOrder order;
-  const unsigned grid = packed_grid(a.tiles, a.heads, &order);
-  constexpr auto kern = packed_fwd_kernel<D, CAUSAL>;
-  const size_t lds = 4 * (size_t)Tile<D>::ELEMS * sizeof(bf16);      // two stages of 64 keys and values
+  const unsigned grid = packed_grid(a.tiles, a.heads, &order) * Split<QW, KG>::PARTS;
+  constexpr auto kern = packed_fwd_kernel<D, CAUSAL, QW, KG>;
+  constexpr size_t lds = KG * 4 * (size_t)Tile<D>::ELEMS * sizeof(bf16), merge = (size_t)(KG - 1) * QW * (D / 32 * 16 + 2) * 64 * sizeof(float);
+  static_assert(merge <= lds && lds <= 160 * 1024, "the merge takes the stages' place");
   if (const int rc = reserve_lds<kern>("attention_packed", lds); rc != CEPHALO_OK) return rc;
-  kern<<<grid, kThreads, lds, s>>>(a, order, qkv, O, lse);
+  kern<<<grid, Split<QW, KG>::THREADS, lds, s>>>(a, order, qkv, O, lse);
   CEPHALO_CHECK_LAUNCH("attention_packed_fwd");
+  return CEPHALO_OK;
+}
+template <int D, bool CAUSAL, int QW, int KG>
+int launch_dq(const PackedArgs& a, const bf16* qkv, const bf16* O, const bf16* dO, const float* lse, float* dvec, bf16* dqkv, hipStream_t s) {
+  PackedOrder order;
+  const unsigned grid = packed_grid(a.tiles, a.heads, &order) * Split<QW, KG>::PARTS;
+  constexpr auto kern = packed_dq_kernel<D, CAUSAL, QW, KG>;
+  constexpr size_t lds = KG * 4 * (size_t)Tile<D>::ELEMS * sizeof(bf16);      // (the merge takes less)
+  if (const int rc = reserve_lds<kern>("attention_packed", lds); rc != CEPHALO_OK) return rc;
+  kern<<<grid, Split<QW, KG>::THREADS, lds, s>>>(a, order, qkv, O, dO, lse, dvec, dqkv);
+  CEPHALO_CHECK_LAUNCH("attention_packed_dq");
+  return CEPHALO_OK;
+}
+// Whether a launch takes the form (2, 2): where 128 queries a block would leave half of the compute units without one (heads up to 64, two of whose blocks
+// share a compute unit: some of them).
+bool halves(const PackedArgs& a, int D) { return (int64_t)a.tiles * a.heads <= (D <= 64 ? 256 : 128); }
+
+template <int D, bool CAUSAL>
+int fwd_cfg(const PackedArgs& a, const bf16* qkv, bf16* O, float* lse, hipStream_t s) {
+  return halves(a, D) ? launch_fwd<D, CAUSAL, 2, 2>(a, qkv, O, lse, s) : launch_fwd<D, CAUSAL, 4, 1>(a, qkv, O, lse, s);
+}
+template <int D, bool CAUSAL>
+int dq_cfg(const PackedArgs& a, const bf16* qkv, const bf16* O, const bf16* dO, const float* lse, float* dvec, bf16* dqkv, hipStream_t s) {
+  return halves(a, D) ? launch_dq<D, CAUSAL, 2, 2>(a, qkv, O, dO, lse, dvec, dqkv, s) : launch_dq<D, CAUSAL, 4, 1>(a, qkv, O, dO, lse, dvec, dqkv, s);
+}
+
+template <int D> int join(const PackedArgs& a, bf16* dqkv, hipStream_t s) {
+  if (a.join_items == 0) return CEPHALO_OK;
+  packed_join_kernel<D><<<dim3(D / 4, a.join_items, a.kv_heads), 256, 0, s>>>(a, dqkv);
+  CEPHALO_CHECK_LAUNCH("attention_packed_join");
   return CEPHALO_OK;
 }
 
 template <int D, bool CAUSAL>
 int bwd_cfg(const PackedArgs& a, const bf16* qkv, const bf16* O, const bf16* dO, const float* lse, float* dvec, bf16* dqkv, hipStream_t s) {
+  // two stages of Q and dO (and, wide, the keys and values) and of the row statistics, or at the end the merge of the halves
+  constexpr size_t stages = (4 * (size_t)Tile<D>::ELEMS + (D <= 64 ? 0 : 2 * (size_t)Tile<D, 128>::ELEMS)) * sizeof(bf16) + 2 * 128 * sizeof(float);
+  constexpr size_t merge = D <= 64 ? 0 : (size_t)4 * (D / 32 * 16 * 2) * 64 * sizeof(float);
+  constexpr size_t lds = stages > merge ? stages : merge;
   PackedOrder order;
-  {
-    const unsigned grid = packed_grid(a.tiles, a.heads, &order);
-    constexpr auto kern = packed_dq_kernel<D, CAUSAL>;
-    const size_t lds = 4 * (size_t)Tile<D>::ELEMS * sizeof(bf16);
-    if (const int rc = reserve_lds<kern>("attention_packed", lds); rc != CEPHALO_OK) return rc;
-    kern<<<grid, kThreads, lds, s>>>(a, order, qkv, O, dO, lse, dvec, dqkv);
-    CEPHALO_CHECK_LAUNCH("attention_packed_dq");
+  const unsigned key_blocks = packed_grid(a.key_items, a.kv_heads, &order);
+  if (packed_one_launch(a.tiles, a.heads, a.kv_heads, a.d)) {
+    PackedOrder by_queries;
+    constexpr int PARTS = Split<D <= 64 ? 2 : 4, 2>::PARTS;
+    const unsigned query_blocks = packed_grid(a.tiles, a.heads, &by_queries) * PARTS;
+    constexpr auto kern = packed_bwd_kernel<D, CAUSAL>;
+    constexpr size_t dq_lds = 8 * (size_t)Tile<D>::ELEMS * sizeof(bf16), most = dq_lds > lds ? dq_lds : lds;
+    if (const int rc = reserve_lds<kern>("attention_packed", most); rc != CEPHALO_OK) return rc;
+    kern<<<key_blocks + query_blocks, kBothThreads<D>, most, s>>>(a, order, by_queries, (int)key_blocks, qkv, O, dO, lse, dqkv);
+    CEPHALO_CHECK_LAUNCH("attention_packed_bwd");
+    return join<D>(a, dqkv, s);
   }
-  const unsigned grid = packed_grid(a.key_items, a.kv_heads, &order);
+  if (const int rc = dq_cfg<D, CAUSAL>(a, qkv, O, dO, lse, dvec, dqkv, s); rc != CEPHALO_OK) return rc;
   if constexpr (D <= 64) {
     constexpr auto kern = packed_dkv_narrow_kernel<D, CAUSAL>;
-    const size_t lds = 4 * (size_t)Tile<D>::ELEMS * sizeof(bf16) + 2 * 128 * sizeof(float);
     if (const int rc = reserve_lds<kern>("attention_packed", lds); rc != CEPHALO_OK) return rc;
-    kern<<<grid, kThreads, lds, s>>>(a, order, qkv, dO, lse, dvec, dqkv);
+    kern<<<key_blocks, kThreads, lds, s>>>(a, order, qkv, dO, lse, dvec, dqkv);
   } else {
     constexpr auto kern = packed_dkv_kernel<D, CAUSAL>;
-    // staging (2 stages of Q and dO, the keys, the values, the row statistics) or, at the end, the merge of the halves
-    const size_t staging = (4 * (size_t)Tile<D>::ELEMS + 2 * (size_t)Tile<D, 128>::ELEMS) * sizeof(bf16) + 2 * 128 * sizeof(float);
-    const size_t merge = (size_t)4 * (D / 32 * 16 * 2) * 64 * sizeof(float);
-    const size_t lds = staging > merge ? staging : merge;
     if (const int rc = reserve_lds<kern>("attention_packed", lds); rc != CEPHALO_OK) return rc;
-    kern<<<grid, kThreads8, lds, s>>>(a, order, qkv, dO, lse, dvec, dqkv);
+    kern<<<key_blocks, kThreads8, lds, s>>>(a, order, qkv, dO, lse, dvec, dqkv);
   }
   CEPHALO_CHECK_LAUNCH("attention_packed_dkv");
-  if (a.join_items > 0) {
-    packed_join_kernel<D><<<dim3(D / 4, a.join_items, a.kv_heads), 256, 0, s>>>(a, dqkv);
-    CEPHALO_CHECK_LAUNCH("attention_packed_join");
-  }
-  return CEPHALO_OK;
+  return join<D>(a, dqkv, s);
 }
 
 }  // namespace

@@ -79,6 +79,22 @@ template <int D, int ROWS = TILE, int THREADS = kThreads> struct Tile {
 #pragma unroll
     for (int j = 0; j < PER_WAVE; ++j) stage_one(rsrc, j, (unsigned)row0 * ld_bytes + col_bytes, ld_bytes, lds, d);
   }
+  // The same with the lanes' parts of the offsets at hand (wave: this wavefront's place among those that stage the tile).
+  __device__ static __forceinline__ void stage_lanes(unsigned (&part)[PER_WAVE], unsigned ld_bytes, int d, int wave) {
+#pragma unroll
+    for (int j = 0; j < PER_WAVE; ++j) {
+      part[j] = stage_lane(j, ld_bytes, d, wave);
+      asm volatile("" : "+v"(part[j]));                    // (kept: formed again for every tile they cost more than the products leave time for)
+    }
+  }
+  __device__ static __forceinline__ void stage_at(i32x4 rsrc, const unsigned (&part)[PER_WAVE], unsigned tile_bytes, lds_bf16* lds, int wave) {
+    if (LOADS < NW && wave >= LOADS) return;
+#pragma unroll
+    for (int j = 0; j < PER_WAVE; ++j) {
+      const unsigned dst = (unsigned)(uintptr_t)(lds + (wave * PER_WAVE + j) * RPL * LD), off = part[j] + tile_bytes;
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" :: "s"(dst), "v"(off), "s"(rsrc) : "m0");
+    }
+  }
   // operand with MFMA rows = tile rows [rb, rb+32), contraction over d in [kk, kk+16)   (rb: a multiple of 16 rows from
   // the tile's first row, so that a row's place in its group of 16 is the lane's)
   __device__ static bf16x8 frag_rows(const lds_bf16* lds, int rb, int kk) {
@@ -128,6 +144,12 @@ template <int D> struct FragAddr {
       lo[k] = base + (cols ^ (unsigned)(k * 64));
       hi[k] = base + (cols ^ (16u * TL::FLIP8) ^ (unsigned)(k * 64));
     }
+  }
+  __device__ __forceinline__ void hold() {               // (the addresses as they are: the compiler would add `first` again at every read)
+#pragma unroll
+    for (int k = 0; k < D / 16; ++k) asm volatile("" : "+v"(r[k]));
+#pragma unroll
+    for (int k = 0; k < D / 32; ++k) asm volatile("" : "+v"(lo[k]), "+v"(hi[k]));
   }
   __device__ __forceinline__ void flip() {
 #pragma unroll
@@ -242,15 +264,16 @@ template <int AT, int PLACES, typename F> __device__ __forceinline__ void spread
 
 // One wavefront's share of a key tile in the forward: 32 queries by 64 keys.  What bounds the kernels built on it and on the two below, and how their
 // products and exponentials are interleaved, stands at the kernels.
-template <int D>
+// BUF: which of the two stages `at` was made for the tile is in (0 where the caller turns `at` instead).
+template <int D, int BUF = 0>
 __device__ __forceinline__ void fwd_tile(const FragAddr<D>& at, const bf16x8 (&qf)[D / 16], f32x16 (&o)[D / 32], float& m_run, float& l_run, float c2,
                                          bool mask, int last) {
   constexpr int NP = D / 16, DT = D / 32, N = 4 * NP, kAhead = 3;
   // S^T of the two blocks of 32 keys, then O^T += V^T P^T of each
   auto fetch = [&](int i) -> bf16x8 {
     const int seg = i / NP, j = i % NP;
-    if (seg < 2) return at.rows(0, seg * 32, j);
-    return at.cols(1, j % DT, (seg - 2) * 32 + 16 * (j / DT));
+    if (seg < 2) return at.rows(2 * BUF, seg * 32, j);
+    return at.cols(2 * BUF + 1, j % DT, (seg - 2) * 32 + 16 * (j / DT));
   };
   bf16x8 f[kAhead], pf[2][2];
   f32x16 s[2], zero;
@@ -323,14 +346,14 @@ __device__ __forceinline__ float row_dot(const bf16* __restrict__ O, int64_t ld,
 }
 
 // One wavefront's share of a key tile in the dQ kernel: 32 queries by 64 keys, as two blocks of 32 keys.
-template <int D>
+template <int D, int BUF = 0>
 __device__ __forceinline__ void dq_tile(const FragAddr<D>& at, const bf16x8 (&qf)[D / 16], const bf16x8 (&dof)[D / 16], f32x16 (&dq)[D / 32],
                                         float c2, float lse2, float dv, bool mask, int last) {
   constexpr int NP = D / 16, N = 6 * NP, kAhead = 3, DT = D / 32;
   auto fetch = [&](int i) -> bf16x8 {
     const int seg = i / NP, j = i % NP;
-    if (seg < 4) return at.rows(seg & 1, seg / 2 * 32, j);
-    return at.cols(0, j % DT, (seg - 4) * 32 + 16 * (j / DT));
+    if (seg < 4) return at.rows(2 * BUF + (seg & 1), seg / 2 * 32, j);
+    return at.cols(2 * BUF, j % DT, (seg - 4) * 32 + 16 * (j / DT));
   };
   bf16x8 f[kAhead], df[2][2];
   f32x16 s[2], dp[2], zero;
@@ -364,7 +387,7 @@ __device__ __forceinline__ void dq_tile(const FragAddr<D>& at, const bf16x8 (&qf
 
 // One wavefront's share of a query tile in the dK / dV kernels that hold their keys in registers: 64 queries by 32 keys.  st: the rows' statistics,
 // -lse / scale and, `dvecs` further on, -dvec, from this half-wavefront's first row on.
-template <int D, bool CAUSAL, int dvecs>
+template <int D, bool CAUSAL, int dvecs, int BUF = 0>
 __device__ __forceinline__ void dkv_tile(const FragAddr<D>& at, const bf16x8 (&kf)[D / 16], const bf16x8 (&vf)[D / 16], f32x16 (&dk)[D / 32], f32x16 (&dvv)[D / 32],
                                          const LDS_AS float* st, float c2, int t0, int t, int qb0) {
   constexpr int NP = D / 16, DT = D / 32, N = 8 * NP, kAhead = 3;
@@ -372,8 +395,8 @@ __device__ __forceinline__ void dkv_tile(const FragAddr<D>& at, const bf16x8 (&k
   // the products: S and dP of the first block and of the second, then dV and dK of each
   auto fetch = [&](int i) -> bf16x8 {
     const int seg = i / NP, j = i % NP;
-    if (seg < 4) return at.rows(seg & 1, seg / 2 * 32, j);
-    return at.cols(1 - (seg & 1), j % DT, (seg - 4) / 2 * 32 + 16 * (j / DT));
+    if (seg < 4) return at.rows(2 * BUF + (seg & 1), seg / 2 * 32, j);
+    return at.cols(2 * BUF + 1 - (seg & 1), j % DT, (seg - 4) / 2 * 32 + 16 * (j / DT));
   };
   f32x16 s[2], dp[2];
   auto start = [&](f32x16& acc, int at) {           // a row's statistic is where its sums start

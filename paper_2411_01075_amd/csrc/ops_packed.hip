@@ -68,14 +68,24 @@ bool all_aligned(std::initializer_list<const void*> ptrs) {
 namespace {
 constexpr int kMostPieces = 1024;      // pieces that a list cuts its keys' walks into, beyond one each
 
-// How many steps of a walk an item takes.  A launch lasts as long as its longest block, and a key tile's walk is as long as the queries that see it times the
-// heads that share it, so few keys and long walks leave the chip idle: walks are cut so that none is longer than an equal share of all steps on the
-// compute units' blocks (256 of eight wavefronts, twice that for heads up to 64; fp32 cuts a tile's keys into eighths first).  A piece pays for its place in the
-// workspace, written and read once more, about as much as two or three steps, hence at least kLeast.
-int steps_an_item(const cephalo_packed_desc* d, int64_t steps) {
-  const bool f32 = d->dtype == CEPHALO_F32;
-  const int64_t blocks = f32 ? 64 : d->head_dim > 64 ? 256 : 512, least = f32 ? 2 : 4;
-  return (int)std::min<int64_t>(std::max((steps * d->kv_heads + blocks - 1) / blocks, least), (int64_t)1 << 30);
+// How many steps of a walk an item takes, and by how many the longest walk may exceed that without any being cut.  A launch lasts as long as its longest block,
+// and a key tile's walk is as long as the queries that see it times the heads that share it, so few keys and long walks leave the chip idle: walks
+// are cut to an equal share of all steps on the blocks that run at once: 256 of eight wavefronts, twice that for heads up to 64 (fp32 cuts a tile's
+// keys into eighths first).  Where the dQ blocks run in the same launch they fill what the longest items leave, so the share is a little longer, and it
+// is one of the blocks that they leave where that is a quarter or more.  Pieces pay for their places in the workspace and for the launch that joins them, as much
+// as five steps or so (fp32, whose steps take longer: 2).  Us of the whole backward, without pieces, in pieces of 8, of 4: 2 x 512 tokens, 4 heads of 64 over 2,
+// causal 44, 26, 16; 8 x 512, 8 over 8: 20, 20, 29; 700 + 300 + 100, 16 of 128 over 4: 95, 33, 43.
+struct Share { int steps, slack; };
+Share steps_an_item(const cephalo_packed_desc* d, int64_t tiles, int64_t steps) {
+  const bool f32 = d->dtype == CEPHALO_F32, wide = d->head_dim > 64;
+  const int64_t all = steps * d->kv_heads, blocks = f32 ? 64 : wide ? 256 : 512;
+  double share = (double)all / blocks;
+  if (!f32 && packed_one_launch(tiles, d->heads, d->kv_heads, d->head_dim)) {
+    const int64_t left = blocks - tiles * d->heads * (wide ? 1 : 2);
+    share *= 1.2;
+    if (left >= blocks / 4) share = std::max(share, (double)all / left);
+  }
+  return {(int)std::min(std::max(std::ceil(share), f32 ? 2.0 : 4.0), 1e9), f32 ? 2 : 5};
 }
 }  // namespace
 
@@ -100,12 +110,14 @@ extern "C" int cephalo_packed_plan(cephalo_packed_desc* d, int32_t samples, cons
   PackedTile* list = static_cast<PackedTile*>(plan);
   const int causal = d->causal, group = d->heads / d->kv_heads;
   int tiles = 0;
-  int64_t steps = 0;
+  int64_t steps = 0, longest_walk = 0;
   for (int i = 0; i < samples; ++i) {
     const int rows = starts[i + 1] - starts[i];
     for (int t = 0; (int64_t)t * kPackedTile < rows; ++t) {
       list[tiles++] = {starts[i], rows, t, 0};
-      steps += (int64_t)walk_steps(causal, rows, t) * group;
+      const int64_t walk = (int64_t)walk_steps(causal, rows, t) * group;
+      steps += walk;
+      longest_walk = std::max(longest_walk, walk);
     }
   }
   std::sort(list, list + tiles, [causal](const PackedTile& a, const PackedTile& b) {
@@ -113,17 +125,18 @@ extern "C" int cephalo_packed_plan(cephalo_packed_desc* d, int32_t samples, cons
     return wa != wb ? wa > wb : a.first != b.first ? a.first < b.first : a.tile < b.tile;
   });
   // the walks, cut; an entry of the list stands for the keys of the same tile
-  const int64_t most = steps_an_item(d, steps);
+  if (longest_walk > (int64_t)1 << 30) return fail(CEPHALO_EUNSUPPORTED, "packed_plan: %d rows under %d heads of a key head", longest, group);
+  const Share share = steps_an_item(d, tiles, steps);
+  const bool cut = longest_walk > (int64_t)share.steps + share.slack;
   int items = 0, joins = 0, slots = 0, spare = kMostPieces;
   auto pieces_of = [&](const PackedTile& e) {
     const int64_t walk = (int64_t)walk_steps(causal, e.rows, e.tile) * group;
-    return walk * 4 > most * 5 ? (int)((walk + most - 1) / most) : 1;
+    return cut && walk * 4 > (int64_t)share.steps * 5 ? (int)((walk + share.steps - 1) / share.steps) : 1;
   };
   KeyItem* keys = reinterpret_cast<KeyItem*>(list + tiles);
   for (int i = 0; i < tiles; ++i) {
     const PackedTile& e = list[i];
     const int64_t walk = (int64_t)walk_steps(causal, e.rows, e.tile) * group;
-    if (walk > (int64_t)1 << 30) return fail(CEPHALO_EUNSUPPORTED, "packed_plan: %d rows under %d heads of a key head", e.rows, group);
     const int pieces = std::min(pieces_of(e), spare + 1);
     spare -= pieces - 1;
     for (int q = 0; q < pieces; ++q)

@@ -27,6 +27,9 @@ struct PackedArgs {
 __host__ __device__ inline int packed_width(int d) { return d <= 32 ? 32 : d <= 64 ? 64 : 128; }      // the tile a head of d columns runs on
 inline size_t packed_part_floats(int d) { return 2 * (size_t)kPackedTile * packed_width(d); }
 
+// Whether the backward is one launch: where its two halves, one after the other, would leave compute units idle.
+inline bool packed_one_launch(int64_t tiles, int heads, int kv_heads, int d) { return tiles * (heads + kv_heads) <= (d <= 64 ? 1536 : 768); }
+
 // Steps of a tile's keys over all the heads that share them, and the first row that sees one.
 __host__ __device__ inline int walk_first(int causal, int tile) { return causal ? tile * kPackedTile : 0; }
 __host__ __device__ inline int walk_steps(int causal, int rows, int tile) { return (rows - walk_first(causal, tile) + kWalkRows - 1) / kWalkRows; }
