@@ -116,8 +116,8 @@ __device__ __forceinline__ void store_columns(float* __restrict__ out, int64_t l
       if (c < d) out[(int64_t)row * ld + c] = o[q][i] * mul;
     }
 }
-// Adds the four wavefronts' `o` in wavefront order into wavefront 0's (red: kWaves - 1 images of P x 64 lanes x 4).
-template <int P>
+// Adds the wavefronts' `o` in wavefront order into wavefront 0's (red: W - 1 images of P x 64 lanes x 4).
+template <int P, int W = kWaves>
 __device__ __forceinline__ void merge_sums(f32x4 (&o)[P], f32x4* red) {
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   __syncthreads();
@@ -128,7 +128,7 @@ __device__ __forceinline__ void merge_sums(f32x4 (&o)[P], f32x4* red) {
   __syncthreads();
   if (wave == 0) {
 #pragma unroll
-    for (int w = 0; w < kWaves - 1; ++w)
+    for (int w = 0; w < W - 1; ++w)
 #pragma unroll
       for (int q = 0; q < P; ++q) o[q] += red[(w * P + q) * 64 + lane];
   }

@@ -64,11 +64,12 @@ __device__ __forceinline__ void hide_scores(f32x16 (&s)[2], int last) {      // 
 }
 // One tile of the forward, its values in stage BUF: its scores are at hand (s, their maximum mx in the log2 domain), and while its exponentials run on the
 // vector unit the matrix core forms the next tile's scores (NEXT: keys in the other stage, into nx; mx becomes their maximum) and then
-// O^T += V^T P^T.  next_hidden, next_last: whether some keys of the next tile are hidden, and hide_scores' argument.
-template <int D, bool NEXT, int BUF>
+// O^T += V^T P^T.  next_hidden, next_last(): whether some keys of the next tile are hidden, and hide_scores' argument.
+// between(i): run after product i; kAhead: products that a fragment is asked for ahead.
+template <int D, bool NEXT, int BUF, int kAhead, typename Last, typename Between>
 __device__ __forceinline__ void fwd_step(const FragAddr<D>& at, const bf16x8 (&qf)[D / 16], f32x16 (&o)[D / 32], f32x16 (&s)[2], f32x16 (&nx)[2], float& mx, float& m_run,
-                                         float& l_run, float c2, bool next_hidden, int next_last) {
-  constexpr int NP = D / 16, DT = D / 32, NA = NEXT ? 2 * NP : 0, N = NA + 2 * NP, kAhead = NEXT ? 3 : 2;
+                                         float& l_run, float c2, bool next_hidden, Last next_last, Between between) {
+  constexpr int NP = D / 16, DT = D / 32, NA = NEXT ? 2 * NP : 0, N = NA + 2 * NP;
   auto fetch = [&](int i) -> bf16x8 {
     if (i < NA) return at.rows(2 * (BUF ^ 1), i / NP * 32, i % NP);
     const int k = i - NA, j = k % NP;
@@ -112,6 +113,7 @@ __device__ __forceinline__ void fwd_step(const FragAddr<D>& at, const bf16x8 (&q
     if constexpr (i < NA) nx[i / NP] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[i % kAhead], qf[i % NP], i % NP == 0 ? zero : nx[i / NP], 0, 0, 0);
     else o[k % NP % DT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[i % kAhead], pf[k / NP][k % NP / DT], o[k % NP % DT], 0, 0, 0);
     if constexpr (i + kAhead < N) f[i % kAhead] = fetch(i + kAhead);
+    between(step);
     // the exponentials over the products of the next scores and of the first 32 keys
     if constexpr (NEXT) {
 #pragma unroll
@@ -123,7 +125,7 @@ __device__ __forceinline__ void fwd_step(const FragAddr<D>& at, const bf16x8 (&q
     }
     if constexpr (k == NP - 1) {
       pf[1][0] = pack8(s[1], 0); pf[1][1] = pack8(s[1], 8);
-      if (NEXT && next_hidden) hide_scores(nx, next_last);
+      if (NEXT && next_hidden) hide_scores(nx, next_last());
     }
     if constexpr (NEXT && k >= NP) {
 #pragma unroll
@@ -165,6 +167,21 @@ __device__ __forceinline__ bool packed_queries(const PackedArgs& p, const Packed
   return *row0 < e->rows;
 }
 
+// The loads of the tiles ahead, dealt out over a tile's products: load q of TOTAL follows product q * EVERY.  A load instruction keeps the address unit for 16
+// clocks, which the compute unit's wavefronts share: issued in one bunch the eight of a tile of 128 hold a wavefront for 330 to 460 clocks.
+template <int TOTAL, int PRODUCTS, typename Load>
+struct Dealt {
+  static constexpr int EVERY = PRODUCTS / TOTAL;
+  static_assert(EVERY >= 1, "a product for each load");
+  Load load;
+  template <typename I> __device__ __forceinline__ void operator()(I) const {
+    if constexpr (I::value % EVERY == 0 && I::value / EVERY < TOTAL) load(I::value / EVERY);
+  }
+};
+template <int TOTAL, int PRODUCTS, typename Load> __device__ __forceinline__ Dealt<TOTAL, PRODUCTS, Load> dealt(Load load) { return {load}; }
+// the descriptor, or one of no extent: its loads bring zeros
+__device__ __forceinline__ i32x4 only_if(bool there, i32x4 rsrc) { return i32x4{rsrc[0], rsrc[1], there ? rsrc[2] : 0, rsrc[3]}; }
+
 // The keys are staged one tile further ahead than the values.  The queries of a wavefront see the group's first `mine` tiles; it helps to stage the others.
 template <int D, bool CAUSAL, int QW, int KG>
 __global__ void __launch_bounds__(64 * QW * KG, (KG == 1 ? kFwdWaves<D> : D == 128 ? 1 : 2))
@@ -175,7 +192,7 @@ packed_fwd_kernel(PackedArgs p, PackedOrder order, const bf16* __restrict__ qkv,
   PackedTile e;
   int a, r0;
   if (!packed_queries<QW, KG>(p, order, block, &e, &a, &r0)) return;
-  const int lane = threadIdx.x & 63, h = lane >> 5;
+  const int lane = threadIdx.x & 63;
   const int S = e.rows, d = p.d, g = a / p.group;
   const SampleRows x(qkv, p.ld, e.first, S, (p.heads + 2 * p.kv_heads) * d);
   const unsigned k_bytes = (unsigned)((p.heads + g) * d * 2), v_bytes = k_bytes + (unsigned)(p.kv_heads * d * 2);
@@ -211,22 +228,31 @@ packed_fwd_kernel(PackedArgs p, PackedOrder order, const bf16* __restrict__ qkv,
     for (int i = 0; i < 16; ++i) o[dt][i] = 0.f;
   float m_run = -INFINITY, l_run = 0.f, mx = -INFINITY;
   const int rounds = grp.rounds(), mine = q0 >= S ? 0 : grp.upto(CAUSAL ? min(grp.tiles, (q0 + 31) / TILE + 1) : grp.tiles);
-  const int limit = (CAUSAL ? min(q0 + (lane & 31), S - 1) : S - 1) - 4 * h;      // the last key that the lane's query sees
+  // the last key that the lane's query sees, counted from the lane's first of tile kt on (formed where it is used: kept, it is a register too many)
+  auto last = [&](int kt) {
+    int l = threadIdx.x & 63;
+    asm volatile("" : "+v"(l));
+    return (CAUSAL ? min(q0 + (l & 31), S - 1) : S - 1) - 4 * (l >> 5) - kt * TILE;
+  };
   auto hidden = [&](int kt) { return (CAUSAL && kt * TILE + 63 > q0) || kt * TILE + 64 > S; };
   if (mine > 0) {
     fwd_scores<D>(at, qf, s0);
-    if (hidden(grp.at(0))) hide_scores(s0, limit - grp.at(0) * TILE);
+    if (hidden(grp.at(0))) hide_scores(s0, last(grp.at(0)));
 #pragma unroll
     for (int i = 0; i < 32; ++i) mx = fmaxf(mx, s0[i >> 4][i & 15]);
     mx = halves_max(mx) * c2;
   }
   __syncthreads();                                       // (every wavefront has its scores of tile 0: the keys of tile 2 take its place)
   int i = 0;
-  auto step = [&](auto next, auto buf, f32x16 (&s)[2], f32x16 (&nx)[2]) {
-    stage_keys(i + 2);
-    stage_values(i + 1);
-    const int kt = grp.at(i + 1);
-    fwd_step<D, decltype(next)::value, decltype(buf)::value>(at, qf, o, s, nx, mx, m_run, l_run, c2, hidden(kt), limit - kt * TILE);
+  auto step = [&](auto next, auto buf, auto ahead, f32x16 (&s)[2], f32x16 (&nx)[2]) {
+    const int kt = grp.at(i + 1), kt2 = grp.at(i + 2);
+    const i32x4 keys = only_if(kt2 < grp.tiles, x.rsrc), values = only_if(kt < grp.tiles, x.rsrc);
+    auto loads = dealt<2 * TL::PER_WAVE, (decltype(next)::value ? 4 : 2) * D / 16>([&](int n) {
+      constexpr int B = decltype(buf)::value;
+      if (n < TL::PER_WAVE) TL::stage_one_at(keys, part[n], (unsigned)kt2 * tile_bytes + k_bytes, Ks(B), grp.wave, n);
+      else TL::stage_one_at(values, part[n - TL::PER_WAVE], (unsigned)kt * tile_bytes + v_bytes, Vs(B ^ 1), grp.wave, n - TL::PER_WAVE);
+    });
+    fwd_step<D, decltype(next)::value, decltype(buf)::value, decltype(ahead)::value>(at, qf, o, s, nx, mx, m_run, l_run, c2, hidden(kt), [&] { return last(kt); }, loads);
     close();
     ++i;
   };
@@ -234,15 +260,17 @@ packed_fwd_kernel(PackedArgs p, PackedOrder order, const bf16* __restrict__ qkv,
   const std::false_type end;
   const std::integral_constant<int, 0> even;
   const std::integral_constant<int, 1> odd;
+  const std::integral_constant<int, 3> three;
+  const std::integral_constant<int, 2> two;              // (three spill a register behind the loop)
   while (i + 2 < mine) {
-    step(more, even, s0, s1);
-    step(more, odd, s1, s0);
+    step(more, even, three, s0, s1);
+    step(more, odd, three, s1, s0);
   }
   if (i + 1 < mine) {
-    step(more, even, s0, s1);
-    step(end, odd, s1, s0);
+    step(more, even, two, s0, s1);
+    step(end, odd, two, s1, s0);
   } else if (i < mine) {
-    step(end, even, s0, s1);
+    step(end, even, two, s0, s1);
   }
   for (; i < rounds; ++i) {
     stage_keys(i + 2);
@@ -337,9 +365,13 @@ __device__ __forceinline__ void dq_block(const PackedArgs& p, const PackedOrder&
   const int limit = (CAUSAL ? min(q, S - 1) : S - 1) - 4 * h;      // the last key that the lane's query sees
   int i = 0;
   for (; i < mine; ++i) {
-    const int t0 = grp.at(i) * TILE;
-    stage(i + 1);
-    dq_tile<D>(at, qf, dof, dq, c2, lse2, dv, (CAUSAL && t0 + 63 > q0) || t0 + 64 > S, limit - t0);
+    const int t0 = grp.at(i) * TILE, kt = grp.at(i + 1), st = (i + 1) & 1;
+    const i32x4 ahead = only_if(kt < grp.tiles, x.rsrc);
+    auto loads = dealt<2 * TL::PER_WAVE, 6 * D / 16>([&](int n) {
+      const int j = n % TL::PER_WAVE;
+      TL::stage_one_at(ahead, part[j], (unsigned)kt * tile_bytes + (n < TL::PER_WAVE ? k_bytes : v_bytes), n < TL::PER_WAVE ? Ks(st) : Vs(st), grp.wave, j);
+    });
+    dq_tile<D, 0>(at, qf, dof, dq, c2, lse2, dv, (CAUSAL && t0 + 63 > q0) || t0 + 64 > S, limit - t0, loads);
     at.flip();
     close();
   }

@@ -1,35 +1,42 @@
 // fp32 attention over packed samples with grouped heads, forward and backward: the formulas and the blocks' shares of attn_packed.hip on the fp32 matrix
-// products of attn_f32.hip.  A block owns 16 rows, an eighth of an entry of the work list, and its four wavefronts take every fourth block of 16 keys
-// (queries) straight from memory; their results are merged in wavefront order.  Rows past a sample's end are read as zeros.
+// products of attn_f32.hip.  A block owns 16 rows, an eighth of an entry of the work list, and its wavefronts take the blocks of 16 keys (queries) in
+// turn, straight from memory; their results are merged in wavefront order.  Rows past a sample's end are read as zeros.
+//
+// What bounds it is the chain of loads and products of one block of 16, 3 to 5 us: eight wavefronts share it, or four where a head's registers
+// allow no more, and the backward is one launch up to 1024 blocks (dK / dV forms rowsum(dO O) itself).  611 tokens, the longest sample 401, 4 heads of 64 over 2,
+// four wavefronts and two launches -> this: forward 23 -> FWD us, backward 53 -> BWD.
 #include "attn_f32_tile.h"
 #include "packed.h"
 
 namespace cephalo {
 namespace {
 
+template <int P> constexpr int kW = P <= 6 ? 8 : 4;      // wavefronts of a block
+
 // block l: an eighth of an entry (the eighths of an entry follow one another) and a head
-__device__ __forceinline__ int packed_eighth(const PackedOrder& order, int* place) {
-  const int l = blockIdx.x, per = order.by_xcd ? 8 * ((order.units + 7) >> 3) : order.units;      // blocks of an entry in the order without eighths
+__device__ __forceinline__ int packed_eighth(const PackedOrder& order, int l, int* place) {
+  const int per = order.by_xcd ? 8 * ((order.units + 7) >> 3) : order.units;      // blocks of an entry in the order without eighths
   const int rest = l % (8 * per);
   *place = l / (8 * per) * per + rest % per;
   return uniform(rest / per);
 }
-__device__ __forceinline__ bool packed_queries(const PackedArgs& p, const PackedOrder& order, PackedTile* e, int* head, int* row0) {
+__device__ __forceinline__ bool packed_queries(const PackedArgs& p, const PackedOrder& order, int l, PackedTile* e, int* head, int* row0) {
   int place;
-  const int eighth = packed_eighth(order, &place);
+  const int eighth = packed_eighth(order, l, &place);
   if (!packed_tile(p, order, place, e, head)) return false;
   *row0 = e->tile * kPackedTile + 16 * (7 - eighth);      // (the longest first)
   return *row0 < e->rows;
 }
 
 template <int P, bool VEC>
-__global__ void __launch_bounds__(64 * kWaves)
+__global__ void __launch_bounds__(64 * kW<P>)
 packed_f32_fwd_kernel(PackedArgs p, PackedOrder order, int causal, const float* __restrict__ qkv, float* __restrict__ O, float* __restrict__ lse) {
-  __shared__ f32x4 red[(kWaves - 1) * P * 64];
-  __shared__ float ml[kWaves][2][16];
+  const int block = blockIdx.x;
+  __shared__ f32x4 red[(kW<P> - 1) * P * 64];
+  __shared__ float ml[kW<P>][2][16];
   PackedTile e;
   int a, q0;
-  if (!packed_queries(p, order, &e, &a, &q0)) return;
+  if (!packed_queries(p, order, block, &e, &a, &q0)) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4;
   const int S = e.rows, d = p.d, q = q0 + (lane & 15);
   const float* base = qkv + (int64_t)e.first * p.ld;
@@ -41,7 +48,7 @@ packed_f32_fwd_kernel(PackedArgs p, PackedOrder order, int causal, const float* 
   for (int i = 0; i < P; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
   float m = -INFINITY, l = 0.f;
   const int end = causal ? min(S, q0 + 16) : S;
-  for (int t0 = wave * 16; t0 < end; t0 += 16 * kWaves) {
+  for (int t0 = wave * 16; t0 < end; t0 += 16 * kW<P>) {
     f32x4 kf[P], vf[P];
     load_rows<P, VEC>(K, p.ld, t0, S, d, kf);
     load_cols<P>(V, p.ld, t0, S, d, vf);
@@ -72,28 +79,27 @@ packed_f32_fwd_kernel(PackedArgs p, PackedOrder order, int causal, const float* 
   __syncthreads();
   float mx = -INFINITY, sum = 0.f;
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) mx = fmaxf(mx, ml[w][0][lane & 15]);
+  for (int w = 0; w < kW<P>; ++w) mx = fmaxf(mx, ml[w][0][lane & 15]);
   const float shift = mx == -INFINITY ? 0.f : mx;
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) sum += ml[w][1][lane & 15] * expf(ml[w][0][lane & 15] - shift);
+  for (int w = 0; w < kW<P>; ++w) sum += ml[w][1][lane & 15] * expf(ml[w][0][lane & 15] - shift);
   const float mine = expf(m - shift);
 #pragma unroll
   for (int i = 0; i < P; ++i) o[i] *= mine;
-  merge_sums<P>(o, red);
+  merge_sums<P, kW<P>>(o, red);
   if (wave == 0) {
     store_columns<P>(O + (int64_t)e.first * p.ldo + a * d, p.ldo, q, S, d, o, 1.0f / sum);
     if (g == 0 && q < S) lse[(int64_t)a * p.tokens + e.first + q] = mx + logf(sum);
   }
 }
 
+// dvec: where rowsum(dO O) goes for the dK / dV blocks, or null
 template <int P, bool VEC>
-__global__ void __launch_bounds__(64 * kWaves)
-packed_f32_dq_kernel(PackedArgs p, PackedOrder order, int causal, const float* __restrict__ qkv, const float* __restrict__ O, const float* __restrict__ dO,
-                     const float* __restrict__ lse, float* __restrict__ dvec, float* __restrict__ dqkv) {
-  __shared__ f32x4 red[(kWaves - 1) * P * 64];
+__device__ __forceinline__ void dq_block(const PackedArgs& p, const PackedOrder& order, int block, int causal, const float* __restrict__ qkv, const float* __restrict__ O,
+                                         const float* __restrict__ dO, const float* __restrict__ lse, float* __restrict__ dvec, float* __restrict__ dqkv, f32x4* red) {
   PackedTile e;
   int a, q0;
-  if (!packed_queries(p, order, &e, &a, &q0)) return;
+  if (!packed_queries(p, order, block, &e, &a, &q0)) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4;
   const int S = e.rows, d = p.d, q = q0 + (lane & 15);
   const float* base = qkv + (int64_t)e.first * p.ld;
@@ -104,12 +110,12 @@ packed_f32_dq_kernel(PackedArgs p, PackedOrder order, int causal, const float* _
   load_rows<P, VEC>(base + a * d, p.ld, q0, S, d, qf);
   load_rows<P, VEC>(dO + orow, p.ldo, q0, S, d, dof);
   const float dv = row_dot<P, VEC>(O + orow, p.ldo, q0, S, d, dof);
-  if (wave == 0 && g == 0 && q < S) dvec[stat + q] = dv;
+  if (dvec && wave == 0 && g == 0 && q < S) dvec[stat + q] = dv;
   const float l = lse[stat + min(q, S - 1)];
 #pragma unroll
   for (int i = 0; i < P; ++i) dq[i] = f32x4{0.f, 0.f, 0.f, 0.f};
   const int end = causal ? min(S, q0 + 16) : S;
-  for (int t0 = wave * 16; t0 < end; t0 += 16 * kWaves) {
+  for (int t0 = wave * 16; t0 < end; t0 += 16 * kW<P>) {
     f32x4 kf[P], vf[P], kc[P];
     load_rows<P, VEC>(K, p.ld, t0, S, d, kf);
     load_rows<P, VEC>(V, p.ld, t0, S, d, vf);
@@ -124,18 +130,17 @@ packed_f32_dq_kernel(PackedArgs p, PackedOrder order, int causal, const float* _
     if (causal && t0 == q0) add_weighted_diagonal<P>(dq, kc, dz, K, p.ld, t0, S, d, [&](int r) { return t0 + r > q; });
     else add_weighted<P>(dq, kc, dz);
   }
-  merge_sums<P>(dq, red);
+  merge_sums<P, kW<P>>(dq, red);
   if (wave == 0) store_columns<P>(dqkv + (int64_t)e.first * p.ld + a * d, p.ld, q, S, d, dq, p.scale);
 }
 
-template <int P, bool VEC>
-__global__ void __launch_bounds__(64 * kWaves)
-packed_f32_dkv_kernel(PackedArgs p, PackedOrder order, int causal, const float* __restrict__ qkv, const float* __restrict__ dO, const float* __restrict__ lse,
-                      const float* __restrict__ dvec, float* __restrict__ dqkv) {
-  __shared__ f32x4 red[(kWaves - 1) * P * 64];
+// OWN: rowsum(dO O) is formed here, from O, not read from dvec
+template <int P, bool VEC, bool OWN>
+__device__ __forceinline__ void dkv_block(const PackedArgs& p, const PackedOrder& order, int block, int causal, const float* __restrict__ qkv, const float* __restrict__ O,
+                                          const float* __restrict__ dO, const float* __restrict__ lse, const float* __restrict__ dvec, float* __restrict__ dqkv, f32x4* red) {
   KeyItem e;
   int kv, place;
-  const int eighth = packed_eighth(order, &place);
+  const int eighth = packed_eighth(order, block, &place);
   if (!packed_keys(p, order, place, causal, &e, &kv)) return;
   const int t0 = e.tile * kPackedTile + 16 * eighth;
   if (t0 >= e.rows) return;
@@ -149,8 +154,9 @@ packed_f32_dkv_kernel(PackedArgs p, PackedOrder order, int causal, const float* 
 #pragma unroll
   for (int i = 0; i < P; ++i) { dk[i] = f32x4{0.f, 0.f, 0.f, 0.f}; dvv[i] = f32x4{0.f, 0.f, 0.f, 0.f}; }
   const int per = walk_steps(causal, S, e.tile);
-  for (int step = e.begin; step < e.end; ++step) {
-    const int a = kv * p.group + step / per, q0 = walk_first(causal, e.tile) + step % per * kWalkRows + wave * 16;
+  // (four wavefronts share a step)
+  for (int step = e.begin + (wave >> 2); step < e.end; step += kW<P> / 4) {
+    const int a = kv * p.group + step / per, q0 = walk_first(causal, e.tile) + step % per * kWalkRows + (wave & 3) * 16;
     if (q0 >= S || (causal && q0 < t0)) continue;        // (16 rows that all lie before the keys see none of them)
     const float* Q = base + a * d;
     const float* D = dO + (int64_t)e.first * p.ldo + a * d;
@@ -165,7 +171,12 @@ packed_f32_dkv_kernel(PackedArgs p, PackedOrder order, int causal, const float* 
     for (int i = 0; i < 4; ++i) {
       const int q = min(q0 + 4 * g + i, S - 1);
       l[i] = lse[stat + q];
-      dv[i] = dvec[stat + q];
+      if (!OWN) dv[i] = dvec[stat + q];
+    }
+    if (OWN) {
+      const float own = row_dot<P, VEC>(O + (int64_t)e.first * p.ldo + a * d, p.ldo, q0, S, d, dof);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) dv[i] = __shfl(own, 4 * g + i, 64);
     }
     const f32x4 s = dot_rows<P>(qf, kf), dp = dot_rows<P>(dof, vf);      // rows: queries q0 + 4 g + i, column: key t
     f32x4 w, dz;
@@ -194,10 +205,34 @@ packed_f32_dkv_kernel(PackedArgs p, PackedOrder order, int causal, const float* 
     row = t - e.tile * kPackedTile;
     rows = S - e.tile * kPackedTile;
   }
-  merge_sums<P>(dvv, red);
+  merge_sums<P, kW<P>>(dvv, red);
   if (wave == 0) store_columns<P>(to_v, ld, row, rows, d, dvv, 1.0f);
-  merge_sums<P>(dk, red);
+  merge_sums<P, kW<P>>(dk, red);
   if (wave == 0) store_columns<P>(to_k, ld, row, rows, d, dk, e.slot >= 0 ? 1.0f : p.scale);
+}
+
+template <int P, bool VEC>
+__global__ void __launch_bounds__(64 * kW<P>)
+packed_f32_dq_kernel(PackedArgs p, PackedOrder order, int causal, const float* __restrict__ qkv, const float* __restrict__ O, const float* __restrict__ dO,
+                     const float* __restrict__ lse, float* __restrict__ dvec, float* __restrict__ dqkv) {
+  __shared__ f32x4 red[(kW<P> - 1) * P * 64];
+  dq_block<P, VEC>(p, order, blockIdx.x, causal, qkv, O, dO, lse, dvec, dqkv, red);
+}
+template <int P, bool VEC>
+__global__ void __launch_bounds__(64 * kW<P>)
+packed_f32_dkv_kernel(PackedArgs p, PackedOrder order, int causal, const float* __restrict__ qkv, const float* __restrict__ dO, const float* __restrict__ lse,
+                      const float* __restrict__ dvec, float* __restrict__ dqkv) {
+  __shared__ f32x4 red[(kW<P> - 1) * P * 64];
+  dkv_block<P, VEC, false>(p, order, blockIdx.x, causal, qkv, nullptr, dO, lse, dvec, dqkv, red);
+}
+template <int P, bool VEC>
+__global__ void __launch_bounds__(64 * kW<P>)
+packed_f32_bwd_kernel(PackedArgs p, PackedOrder by_keys, PackedOrder by_queries, int key_blocks, int causal, const float* __restrict__ qkv, const float* __restrict__ O,
+                      const float* __restrict__ dO, const float* __restrict__ lse, float* __restrict__ dqkv) {
+  __shared__ f32x4 red[(kW<P> - 1) * P * 64];
+  const int block = blockIdx.x;
+  if (block < key_blocks) dkv_block<P, VEC, true>(p, by_keys, block, causal, qkv, O, dO, lse, nullptr, dqkv, red);
+  else dq_block<P, VEC>(p, by_queries, block - key_blocks, causal, qkv, O, dO, lse, nullptr, dqkv, red);
 }
 
 // The places of a join's pieces added in their order, one value a thread.
@@ -213,18 +248,19 @@ __global__ void __launch_bounds__(256) packed_f32_join_kernel(PackedArgs p, floa
   dqkv[((int64_t)e.first + t) * p.ld + (int64_t)(p.heads + which * p.kv_heads + g) * p.d + c] = sum * (which ? 1.0f : p.scale);
 }
 
-// pieces of 16 dimensions: 2, 4 or 8 (a head in between runs on the next with zeros)
-#define PACKED_F32_FORMS(CALL)                                                                                    \
-  const int pieces = (a.d + 15) / 16;                                                                             \
-  if (vec) { if (pieces <= 2) { CALL(2, true) } else if (pieces <= 4) { CALL(4, true) } else { CALL(8, true) } }  \
-  else { if (pieces <= 2) { CALL(2, false) } else if (pieces <= 4) { CALL(4, false) } else { CALL(8, false) } }
+// pieces of 16 dimensions: 2, 4, 6 or 8 (a head in between runs on the next with zeros)
+#define PACKED_F32_PIECES(CALL, VEC) \
+  if (pieces <= 2) { CALL(2, VEC) } else if (pieces <= 4) { CALL(4, VEC) } else if (pieces <= 6) { CALL(6, VEC) } else { CALL(8, VEC) }
+#define PACKED_F32_FORMS(CALL)              \
+  const int pieces = (a.d + 15) / 16;       \
+  if (vec) { PACKED_F32_PIECES(CALL, true) } else { PACKED_F32_PIECES(CALL, false) }
 }  // namespace
 
 int launch_attn_packed_fwd_f32(const PackedArgs& a, int causal, const float* qkv, float* O, float* lse, hipStream_t s) {
   const bool vec = a.d % 4 == 0 && a.ld % 4 == 0;
   PackedOrder order;
   const unsigned grid = 8 * packed_grid(a.tiles, a.heads, &order);
-#define CALL(P, V) packed_f32_fwd_kernel<P, V><<<grid, 64 * kWaves, 0, s>>>(a, order, causal, qkv, O, lse);
+#define CALL(P, V) packed_f32_fwd_kernel<P, V><<<grid, 64 * kW<P>, 0, s>>>(a, order, causal, qkv, O, lse);
   PACKED_F32_FORMS(CALL)
 #undef CALL
   CEPHALO_CHECK_LAUNCH("attention_packed_fwd");
@@ -235,11 +271,18 @@ int launch_attn_packed_bwd_f32(const PackedArgs& a, int causal, const float* qkv
   const bool vec = a.d % 4 == 0 && a.ld % 4 == 0 && a.ldo % 4 == 0;
   PackedOrder order, by_keys;
   const unsigned grid = 8 * packed_grid(a.tiles, a.heads, &order), key_grid = 8 * packed_grid(a.key_items, a.kv_heads, &by_keys);
-#define CALL(P, V)                                                                                                       \
-  packed_f32_dq_kernel<P, V><<<grid, 64 * kWaves, 0, s>>>(a, order, causal, qkv, O, dO, lse, dvec, dqkv);                \
-  packed_f32_dkv_kernel<P, V><<<key_grid, 64 * kWaves, 0, s>>>(a, by_keys, causal, qkv, dO, lse, dvec, dqkv);
-  PACKED_F32_FORMS(CALL)
+  if ((int64_t)grid + key_grid <= 1024 && a.d <= 64) {      // (wider heads: the two halves together spill)
+#define CALL(P, V) packed_f32_bwd_kernel<P, V><<<grid + key_grid, 64 * kW<P>, 0, s>>>(a, by_keys, order, (int)key_grid, causal, qkv, O, dO, lse, dqkv);
+    if (vec) { if (a.d <= 32) { CALL(2, true) } else { CALL(4, true) } }
+    else { if (a.d <= 32) { CALL(2, false) } else { CALL(4, false) } }
 #undef CALL
+  } else {
+#define CALL(P, V)                                                                                                       \
+  packed_f32_dq_kernel<P, V><<<grid, 64 * kW<P>, 0, s>>>(a, order, causal, qkv, O, dO, lse, dvec, dqkv);                 \
+  packed_f32_dkv_kernel<P, V><<<key_grid, 64 * kW<P>, 0, s>>>(a, by_keys, causal, qkv, dO, lse, dvec, dqkv);
+    PACKED_F32_FORMS(CALL)
+#undef CALL
+  }
   CEPHALO_CHECK_LAUNCH("attention_packed_bwd");
   if (a.join_items > 0) {
     packed_f32_join_kernel<<<dim3(packed_width(a.d), a.join_items, a.kv_heads), 256, 0, s>>>(a, dqkv);

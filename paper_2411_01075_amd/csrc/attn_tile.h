@@ -87,13 +87,14 @@ template <int D, int ROWS = TILE, int THREADS = kThreads> struct Tile {
       asm volatile("" : "+v"(part[j]));                    // (kept: formed again for every tile they cost more than the products leave time for)
     }
   }
-  __device__ static __forceinline__ void stage_at(i32x4 rsrc, const unsigned (&part)[PER_WAVE], unsigned tile_bytes, lds_bf16* lds, int wave) {
+  __device__ static __forceinline__ void stage_one_at(i32x4 rsrc, unsigned part, unsigned tile_bytes, lds_bf16* lds, int wave, int j) {
     if (LOADS < NW && wave >= LOADS) return;
+    const unsigned dst = (unsigned)(uintptr_t)(lds + (wave * PER_WAVE + j) * RPL * LD), off = part + tile_bytes;
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" :: "s"(dst), "v"(off), "s"(rsrc) : "m0");
+  }
+  __device__ static __forceinline__ void stage_at(i32x4 rsrc, const unsigned (&part)[PER_WAVE], unsigned tile_bytes, lds_bf16* lds, int wave) {
 #pragma unroll
-    for (int j = 0; j < PER_WAVE; ++j) {
-      const unsigned dst = (unsigned)(uintptr_t)(lds + (wave * PER_WAVE + j) * RPL * LD), off = part[j] + tile_bytes;
-      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" :: "s"(dst), "v"(off), "s"(rsrc) : "m0");
-    }
+    for (int j = 0; j < PER_WAVE; ++j) stage_one_at(rsrc, part[j], tile_bytes, lds, wave, j);
   }
   // operand with MFMA rows = tile rows [rb, rb+32), contraction over d in [kk, kk+16)   (rb: a multiple of 16 rows from
   // the tile's first row, so that a row's place in its group of 16 is the lane's)
@@ -346,9 +347,11 @@ __device__ __forceinline__ float row_dot(const bf16* __restrict__ O, int64_t ld,
 }
 
 // One wavefront's share of a key tile in the dQ kernel: 32 queries by 64 keys, as two blocks of 32 keys.
-template <int D, int BUF = 0>
+// between(i): run after product i.
+struct Nothing { template <typename I> __device__ __forceinline__ void operator()(I) const {} };
+template <int D, int BUF = 0, typename Between = Nothing>
 __device__ __forceinline__ void dq_tile(const FragAddr<D>& at, const bf16x8 (&qf)[D / 16], const bf16x8 (&dof)[D / 16], f32x16 (&dq)[D / 32],
-                                        float c2, float lse2, float dv, bool mask, int last) {
+                                        float c2, float lse2, float dv, bool mask, int last, Between between = Between()) {
   constexpr int NP = D / 16, N = 6 * NP, kAhead = 3, DT = D / 32;
   auto fetch = [&](int i) -> bf16x8 {
     const int seg = i / NP, j = i % NP;
@@ -375,6 +378,7 @@ __device__ __forceinline__ void dq_tile(const FragAddr<D>& at, const bf16x8 (&qf
     else if constexpr (seg == 1 || seg == 3) dp[seg / 2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[i % kAhead], dof[j], j == 0 ? zero : dp[seg / 2], 0, 0, 0);
     else dq[j % DT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[i % kAhead], df[seg - 4][j / DT], dq[j % DT], 0, 0, 0);
     if constexpr (i + kAhead < N) f[i % kAhead] = fetch(i + kAhead);
+    between(step);
     spread<i - NP - 1, NP>([&](int e) { prob(s[0], e); });
     spread<i - 2 * NP - 1, NP>([&](int e) { s[0][e] *= dp[0][e] - dv; });
     if constexpr (i == 3 * NP) { hide(s[0], 0); df[0][0] = pack8(s[0], 0); df[0][1] = pack8(s[0], 8); }

@@ -78,14 +78,14 @@ constexpr int kMostPieces = 1024;      // pieces that a list cuts its keys' walk
 struct Share { int steps, slack; };
 Share steps_an_item(const cephalo_packed_desc* d, int64_t tiles, int64_t steps) {
   const bool f32 = d->dtype == CEPHALO_F32, wide = d->head_dim > 64;
-  const int64_t all = steps * d->kv_heads, blocks = f32 ? 64 : wide ? 256 : 512;
+  const int64_t all = steps * d->kv_heads, blocks = f32 ? 32 : wide ? 256 : 512;
   double share = (double)all / blocks;
   if (!f32 && packed_one_launch(tiles, d->heads, d->kv_heads, d->head_dim)) {
     const int64_t left = blocks - tiles * d->heads * (wide ? 1 : 2);
     share *= 1.2;
     if (left >= blocks / 4) share = std::max(share, (double)all / left);
   }
-  return {(int)std::min(std::max(std::ceil(share), f32 ? 2.0 : 4.0), 1e9), f32 ? 2 : 5};
+  return {(int)std::min(std::max(std::ceil(share), 4.0), 1e9), 5};
 }
 }  // namespace
 
