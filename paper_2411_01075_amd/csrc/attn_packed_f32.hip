@@ -3,8 +3,8 @@
 // turn, straight from memory; their results are merged in wavefront order.  Rows past a sample's end are read as zeros.
 //
 // What bounds it is the chain of loads and products of one block of 16, 3 to 5 us: eight wavefronts share it, or four where a head's registers
-// allow no more, and the backward is one launch up to 1024 blocks (dK / dV forms rowsum(dO O) itself).  611 tokens, the longest sample 401, 4 heads of 64 over 2,
-// four wavefronts and two launches -> this: forward 23 -> FWD us, backward 53 -> BWD.
+// allow no more, and the backward of heads up to 64 is one launch up to 1024 blocks (dK / dV forms rowsum(dO O) itself).  611 tokens, the longest sample 401, 4 heads of 64 over 2,
+// four wavefronts and two launches -> this: forward 23 -> 17 us, backward 53 -> 33 (with its join).
 #include "attn_f32_tile.h"
 #include "packed.h"
 

@@ -43,6 +43,16 @@ __device__ __forceinline__ void store_vec(T* p, const float (&in)[Vec<T>::N]) {
   *reinterpret_cast<typename Vec<T>::raw*>(p) = r;
 }
 
+// The same past the caches where STREAM (for results that no cache holds anyway).  (A choice at run time loses the hint.)
+template <typename T, bool STREAM>
+__device__ __forceinline__ void store_vec_past(T* p, const float (&in)[Vec<T>::N]) {
+  typename Vec<T>::raw r;
+#pragma unroll
+  for (int i = 0; i < Vec<T>::N; ++i) r[i] = (T)in[i];
+  if constexpr (STREAM) __builtin_nontemporal_store(r, reinterpret_cast<typename Vec<T>::raw*>(p));
+  else *reinterpret_cast<typename Vec<T>::raw*>(p) = r;
+}
+
 __device__ __forceinline__ float wave_sum(float v) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
