@@ -138,6 +138,37 @@ def test_long_samples():
     _check(Packed("bf16", 2, 1, 64, False, [1, 2111]))
 
 
+FULL = [700, 333, 129, 1, 600, 0, 260]                      # 20 tiles of 128 rows
+FULLER = FULL + [640, 697, 512]                             # 35
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("dtype,heads,kv_heads,d,lengths", [
+    ("bf16", 32, 8, 128, FULL), ("bf16", 32, 8, 104, FULL), ("bf16", 40, 8, 64, FULLER), ("bf16", 40, 8, 24, FULLER),
+    ("bf16", 40, 1, 128, FULL), ("bf16", 80, 1, 64, FULL), ("f32", 16, 4, 64, FULL), ("f32", 16, 4, 100, FULL), ("f32", 16, 1, 40, FULL)])
+def test_launches_that_fill_the_chip(dtype, heads, kv_heads, d, lengths, causal):
+    """More blocks than compute units: 128 queries a block and a backward in two launches, where the small calls above split blocks and take one."""
+    print("packed full", dtype, heads, kv_heads, d, causal, flush=True)
+    c = Packed(dtype, heads, kv_heads, d, causal, lengths, before=2, behind=5, gap=8, seed=heads + d)
+    tiles = sum((n + 127) // 128 for n in lengths)
+    assert c.desc.tiles == tiles
+    if dtype == "bf16":
+        assert tiles * heads > 256 and tiles * (heads + kv_heads) > (1536 if d <= 64 else 768)
+    assert kv_heads > 1 or c.desc.joins > 0
+    _check(c)
+    eager = [t.clone() for t in (c.O, c.lse, c.dqkv)]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        c.forward(); c.backward()
+    for _ in range(3):
+        for t in (c.O, c.lse, c.dqkv):
+            t.fill_(MARK)
+        c.workspace.fill_(0xCD)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(eager, (c.O, c.lse, c.dqkv)))
+
+
 def test_rows_far_apart_pass_32_bits():
     """Rows of 2 MiB: the samples lie behind 4 GiB, in the projection and in its gradient."""
     heads, kv_heads, d, pitch, first, lengths = 4, 2, 64, 1 << 20, 2090, [70, 30]
