@@ -345,7 +345,9 @@ int cephalo_op_attention_bwd(const cephalo_layer_desc* desc, const void* qkv, co
  * a / (heads / kv_heads), so that kv_heads = heads is the form above and kv_heads = 1 shares one key head.
  * Attention stays inside a sample: query row q of it sees its rows t <= q (causal) or all of them.  Samples may have any
  * length, 0 and 1 too.  No sample's values reach another's results, not-a-numbers and infinities included.  Rows that belong
- * to no sample are neither read nor written, and neither are columns past a row's width. */
+ * to no sample are neither read nor written, and neither are columns past a row's width.  Inside a sample a row that the causal
+ * mask hides has a weight of zero, which in BF16 mode does not silence an infinity or a not-a-number: it can reach the rows
+ * less than 128 away.  In F32 mode hidden rows are left out. */
 typedef struct cephalo_packed_desc {
   int32_t heads, kv_heads;   /* heads is a multiple of kv_heads */
   int32_t head_dim;          /* up to 128, in BF16 mode a multiple of 8 */
@@ -368,8 +370,10 @@ int cephalo_packed_plan(cephalo_packed_desc* desc, int32_t samples, const int32_
 
 /* Forward: O [tokens, o_pitch] and lse [heads, tokens] fp32, the log-sum-exp of each query row's scaled, masked scores.
  * Backward: dqkv [tokens, qkv_pitch] from dO and what the forward wrote; the sums over the query heads that share a key head are formed
- * in 32 bits, in a fixed order (reproducible).  workspace: device, cephalo_op_attention_packed_bwd_workspace(desc) bytes (0: a desc
- * that the calls refuse); no two calls that overlap in time may share it.  plan, qkv, O, dO, lse, dqkv: device, 16-byte aligned. */
+ * in 32 bits, in an order that the list fixes: the same call gives the same bits.  (The list divides the work by all samples of
+ * the batch, so a sample's last bits go by its neighbours' lengths.)  workspace: device,
+ * cephalo_op_attention_packed_bwd_workspace(desc) bytes (0: a desc that the calls refuse); no two calls that overlap in time may
+ * share it.  plan, qkv, O, dO, lse, dqkv: device, 16-byte aligned.  What a call writes overlaps nothing that it reads. */
 int cephalo_op_attention_packed_fwd(const cephalo_packed_desc* desc, const void* plan, const void* qkv, void* O, float* lse, void* stream);
 size_t cephalo_op_attention_packed_bwd_workspace(const cephalo_packed_desc* desc);
 int cephalo_op_attention_packed_bwd(const cephalo_packed_desc* desc, const void* plan, const void* qkv, const void* O, const void* dO,

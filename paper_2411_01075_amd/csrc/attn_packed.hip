@@ -16,7 +16,6 @@ namespace {
 
 constexpr int kThreads8 = 512;
 
-
 // one sample's rows of the packed projection, and of O or dO
 struct SampleRows {
   const bf16* base;
@@ -34,6 +33,12 @@ template <int D> constexpr int kDqWaves = D == 32 ? 4 : D == 64 ? 3 : 2;
 template <int D> constexpr int kDkvWaves = D == 32 ? 3 : 2;
 
 // ------------------------------------------------------------------------------------ forward
+// What bounds it.  For heads of 128 a tile of 64 keys gives each wavefront 32 products of 32 x 32 x 16 (17 to 21 ns each, by the chip's power), one KiB of LDS
+// for each, and 32 exponentials a lane.  LDS gives 128 bytes a clock to four SIMDs, just what the products take, and the tiles' arrival is a quarter more.
+// A wavefront alone on its SIMD issues an instruction of the vector unit every 8 clocks, two together one every 4, so the exponentials have to run
+// under products: the next tile's scores are formed while this tile's exponentials run.  Against the attention of equal samples, which works on one tile at
+// a time, in TFLOP/s: 8192 tokens, 32 heads of 128, no mask 1078 -> 1138, causal 870 -> 1049; 32 heads of 64, causal 879 -> 949 (a large matrix
+// product of this library reaches 1340).
 __device__ __forceinline__ float halves_max(float v) {      // of lanes l and l ^ 32
   const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, v), __builtin_bit_cast(unsigned, v), false, false);
   return fmaxf(__builtin_bit_cast(float, r[0]), __builtin_bit_cast(float, r[1]));
@@ -400,11 +405,11 @@ __device__ __forceinline__ void dq_block(const PackedArgs& p, const PackedOrder&
   store_transposed<D>(dq, dqkv + (int64_t)e.first * p.ld + a * d, p.ld, q, S, p.scale, d);
 }
 
-template <int D, bool CAUSAL, int QW, int KG>
-__global__ void __launch_bounds__(64 * QW * KG, (KG == 1 ? kDqWaves<D> : D == 128 ? 1 : 2))
+template <int D, bool CAUSAL>
+__global__ void __launch_bounds__(kThreads, kDqWaves<D>)
 packed_dq_kernel(PackedArgs p, PackedOrder order, const bf16* __restrict__ qkv, const bf16* __restrict__ O, const bf16* __restrict__ dO,
                  const float* __restrict__ lse, float* __restrict__ dvec, bf16* __restrict__ dqkv) {
-  dq_block<D, CAUSAL, QW, KG>(p, order, blockIdx.x, qkv, O, dO, lse, dvec, dqkv);
+  dq_block<D, CAUSAL, 4, 1>(p, order, blockIdx.x, qkv, O, dO, lse, dvec, dqkv);
 }
 
 // The queries that a block of 128 keys walks: of each of the group's heads the tiles of 64 that see the keys, from step `begin` of that order on.
@@ -753,28 +758,26 @@ int launch_fwd(const PackedArgs& a, const bf16* qkv, bf16* O, float* lse, hipStr
   CEPHALO_CHECK_LAUNCH("attention_packed_fwd");
   return CEPHALO_OK;
 }
-template <int D, bool CAUSAL, int QW, int KG>
+template <int D, bool CAUSAL>
 int launch_dq(const PackedArgs& a, const bf16* qkv, const bf16* O, const bf16* dO, const float* lse, float* dvec, bf16* dqkv, hipStream_t s) {
   PackedOrder order;
-  const unsigned grid = packed_grid(a.tiles, a.heads, &order) * Split<QW, KG>::PARTS;
-  constexpr auto kern = packed_dq_kernel<D, CAUSAL, QW, KG>;
-  constexpr size_t lds = KG * 4 * (size_t)Tile<D>::ELEMS * sizeof(bf16);      // (the merge takes less)
+  const unsigned grid = packed_grid(a.tiles, a.heads, &order);
+  constexpr auto kern = packed_dq_kernel<D, CAUSAL>;
+  constexpr size_t lds = 4 * (size_t)Tile<D>::ELEMS * sizeof(bf16);
   if (const int rc = reserve_lds<kern>("attention_packed", lds); rc != CEPHALO_OK) return rc;
-  kern<<<grid, Split<QW, KG>::THREADS, lds, s>>>(a, order, qkv, O, dO, lse, dvec, dqkv);
+  kern<<<grid, kThreads, lds, s>>>(a, order, qkv, O, dO, lse, dvec, dqkv);
   CEPHALO_CHECK_LAUNCH("attention_packed_dq");
   return CEPHALO_OK;
 }
-// Whether a launch takes the form (2, 2): where 128 queries a block would leave half of the compute units without one (heads up to 64, two of whose blocks
-// share a compute unit: some of them).
+// Whether a forward takes the form (2, 2): where 128 queries a block would leave half of the compute units without one (heads up to 64, two of whose blocks
+// share a compute unit: some of them).  Us of the forward, (4, 1) and (2, 2), by list entries times heads.  Heads of 128: 64: 21 and 16; 128: 21 and 17;
+// 256: 24 and 25 (2 x 1024 tokens), 36 and 34 (2048, 16 key heads); 384: 42 and 50; 512 (8 x 512, no mask): 26 and 45.  Heads of 64: 32: 10.4 and 8.3;
+// 256: 26 and 20 (2048 tokens), 10.6 and 9.0 (8 x 512); 384: 13.8 and 16.1; 512: 10.9 and 14.5.
 bool halves(const PackedArgs& a, int D) { return (int64_t)a.tiles * a.heads <= (D <= 64 ? 256 : 128); }
 
 template <int D, bool CAUSAL>
 int fwd_cfg(const PackedArgs& a, const bf16* qkv, bf16* O, float* lse, hipStream_t s) {
   return halves(a, D) ? launch_fwd<D, CAUSAL, 2, 2>(a, qkv, O, lse, s) : launch_fwd<D, CAUSAL, 4, 1>(a, qkv, O, lse, s);
-}
-template <int D, bool CAUSAL>
-int dq_cfg(const PackedArgs& a, const bf16* qkv, const bf16* O, const bf16* dO, const float* lse, float* dvec, bf16* dqkv, hipStream_t s) {
-  return halves(a, D) ? launch_dq<D, CAUSAL, 2, 2>(a, qkv, O, dO, lse, dvec, dqkv, s) : launch_dq<D, CAUSAL, 4, 1>(a, qkv, O, dO, lse, dvec, dqkv, s);
 }
 
 template <int D> int join(const PackedArgs& a, bf16* dqkv, hipStream_t s) {
@@ -803,7 +806,7 @@ int bwd_cfg(const PackedArgs& a, const bf16* qkv, const bf16* O, const bf16* dO,
     CEPHALO_CHECK_LAUNCH("attention_packed_bwd");
     return join<D>(a, dqkv, s);
   }
-  if (const int rc = dq_cfg<D, CAUSAL>(a, qkv, O, dO, lse, dvec, dqkv, s); rc != CEPHALO_OK) return rc;
+  if (const int rc = launch_dq<D, CAUSAL>(a, qkv, O, dO, lse, dvec, dqkv, s); rc != CEPHALO_OK) return rc;
   if constexpr (D <= 64) {
     constexpr auto kern = packed_dkv_narrow_kernel<D, CAUSAL>;
     if (const int rc = reserve_lds<kern>("attention_packed", lds); rc != CEPHALO_OK) return rc;

@@ -27,7 +27,9 @@ struct PackedArgs {
 __host__ __device__ inline int packed_width(int d) { return d <= 32 ? 32 : d <= 64 ? 64 : 128; }      // the tile a head of d columns runs on
 inline size_t packed_part_floats(int d) { return 2 * (size_t)kPackedTile * packed_width(d); }
 
-// Whether the backward is one launch: where its two halves, one after the other, would leave compute units idle.
+// Whether the bf16 backward is one launch: where its two halves, one after the other, would leave compute units idle.  Us in two and in one, by tiles times
+// (heads + key heads).  Heads of 64: 48: 26 and 16; 320: 68 and 53; 512: 28 and 21; 640: 36 and 36; 768: 41 and 35; 1024: 32 and 32.  Heads of 128: 128: 54
+// and 37; 320: 83 and 63; 512: 112 and 91; 640: 308 and 279; 1024: 88 and 101; 1280: 526 and 548.  (Two: dQ blocks of 128 queries.)
 inline bool packed_one_launch(int64_t tiles, int heads, int kv_heads, int d) { return tiles * (heads + kv_heads) <= (d <= 64 ? 1536 : 768); }
 
 // Steps of a tile's keys over all the heads that share them, and the first row that sees one.
