@@ -353,7 +353,7 @@ typedef struct cephalo_packed_desc {
   int32_t head_dim;          /* up to 128, in BF16 mode a multiple of 8 */
   int32_t causal;            /* 0 or 1 */
   int32_t dtype;             /* CEPHALO_F32 or CEPHALO_BF16 */
-  float   scale;             /* of the scores; 0: 1/sqrt(head_dim) */
+  float   scale;             /* of the scores, 1e-30 to 1e30; 0: 1/sqrt(head_dim) */
   int64_t tokens;            /* rows of qkv, O, dO and dqkv, columns of lse; below 2^31 */
   int64_t qkv_pitch, o_pitch;/* elements from one row of qkv (dqkv) and of O (dO) to the next; in BF16 mode multiples of 8 */
   int32_t samples, longest, tiles, key_items, joins, slots;   /* these and plan_bytes: written by cephalo_packed_plan */

@@ -24,7 +24,8 @@ int check_packed(const char* who, const cephalo_packed_desc* d) {
   const bool bf = d->dtype == CEPHALO_BF16;
   if (bf && d->head_dim % 8 != 0) return fail(CEPHALO_EUNSUPPORTED, "%s: bf16 needs a head dim that is a multiple of 8, got %d", who, d->head_dim);
   if (d->causal != 0 && d->causal != 1) return fail(CEPHALO_EINVAL, "%s: causal must be 0 or 1", who);
-  if (!(d->scale >= 0.f) || !std::isfinite(d->scale)) return fail(CEPHALO_EINVAL, "%s: scale %g must be positive, or 0 for 1/sqrt(head dim)", who, d->scale);
+  // (the kernels hold scale * log2(e) and, of some heads, lse / scale in 32 bits)
+  if (d->scale != 0.f && !(d->scale >= 1e-30f && d->scale <= 1e30f)) return fail(CEPHALO_EINVAL, "%s: scale %g must lie in 1e-30 to 1e30, or be 0 for 1/sqrt(head dim)", who, d->scale);
   if (d->tokens <= 0 || d->tokens >= kRows) return fail(CEPHALO_EINVAL, "%s: %lld rows", who, (long long)d->tokens);
   const int64_t o = (int64_t)d->heads * d->head_dim, qkv = o + 2 * (int64_t)d->kv_heads * d->head_dim;
   if (d->qkv_pitch < qkv || d->o_pitch < o)

@@ -124,6 +124,12 @@ def test_a_scale_of_the_caller_s_and_sharp_scores(heads, kv_heads, d):
     _check(Packed("f32", heads, kv_heads, d, False, [333, 100], scale=0.37))
 
 
+@pytest.mark.parametrize("dtype,d", [("bf16", 32), ("bf16", 64), ("bf16", 128), ("f32", 64)])
+def test_the_smallest_scale(dtype, d):
+    """Scores of nearly zero: every key counts alike, and the gradients of the scores' factors are of the scale's size."""
+    _check(Packed(dtype, 4, 2, d, True, [333, 100], scale=1e-30))
+
+
 @pytest.mark.parametrize("dtype,heads,kv_heads,d", [("bf16", 16, 1, 128), ("bf16", 16, 1, 64), ("bf16", 10, 2, 24), ("f32", 8, 1, 64), ("f32", 6, 1, 50)])
 @pytest.mark.parametrize("causal", [True, False])
 def test_walks_in_pieces(dtype, heads, kv_heads, d, causal):

@@ -250,3 +250,14 @@ def test_the_binding_refuses_tensors_that_are_too_small_or_of_another_type():
         C.cephalo_op_dropout_bwd(C.F32, x, x, 17, 0.1, 1)
     with pytest.raises(C.CephaloError, match="expected"):
         C.cephalo_op_rotary_axes(C.F32, x, 8, x, 8, torch.zeros(2, 1, dtype=torch.int64), 2, [8], 1, 8)
+
+
+@pytest.mark.parametrize("scale", [-0.5, 1e-39, 9e-31, 1.1e30, 3e38, float("inf"), float("nan")])
+def test_scales_whose_products_pass_32_bits_are_refused(scale):
+    with pytest.raises(C.CephaloError):
+        C.cephalo_packed_plan(C.packed_desc(2, 2, 64, True, C.BF16, 8, scale=scale), [0, 8])
+
+
+@pytest.mark.parametrize("scale", [0.0, 1e-30, 1e30])
+def test_scales_at_the_ends_are_taken(scale):
+    C.cephalo_packed_plan(C.packed_desc(2, 2, 64, True, C.BF16, 8, scale=scale), [0, 8])
