@@ -41,7 +41,8 @@ template <int D> constexpr int kDkvWaves = D == 32 ? 3 : 2;
 // product of this library reaches 1340).
 __device__ __forceinline__ float halves_max(float v) {      // of lanes l and l ^ 32
   const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, v), __builtin_bit_cast(unsigned, v), false, false);
-  return fmaxf(__builtin_bit_cast(float, r[0]), __builtin_bit_cast(float, r[1]));
+  const unsigned low = r[0], high = r[1];                // (values of their own: a bit cast of a vector's element takes the vector's first)
+  return fmaxf(__builtin_bit_cast(float, low), __builtin_bit_cast(float, high));
 }
 // S^T of the 64 keys of the first stage and a wavefront's 32 queries
 template <int D>

@@ -435,3 +435,24 @@ def test_the_attention_half_of_a_layer_forward_and_backward():
     for name, got, want in (("out", out, out64), ("dqkv", dqkv, grad)):
         off = np.abs(got.double().cpu().numpy() - want)
         assert off.max() <= 1e-4 * np.abs(want).max() and off.mean() <= 1e-4 * np.abs(want).mean(), (name, off.max(), off.mean())
+
+
+# ---- the largest score ------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype,heads,kv_heads,d,rows", [("bf16", 2, 1, 32, 150), ("bf16", 2, 1, 64, 150), ("bf16", 2, 2, 128, 150), ("bf16", 40, 10, 64, 1100), ("bf16", 20, 5, 128, 1100), ("f32", 2, 1, 64, 150)])
+@pytest.mark.parametrize("causal", [True, False])
+def test_the_largest_score_in_any_place_of_a_tile(dtype, heads, kv_heads, d, rows, causal):
+    """One key whose score is 300 above all others', in each place of 16 and in several tiles: rows that see it take its values.  (Weights e^-300: zero in 32 bits.)"""
+    for place in list(range(16)) + [16 + 5, 64 + 12, 128 + 3]:
+        c = Packed(dtype, heads, kv_heads, d, causal, [rows], scale=1.0)
+        x = torch.zeros(rows, heads + 2 * kv_heads, d, dtype=TORCH[dtype], device="cuda")
+        x[:, :heads, 3], x[place, heads:heads + kv_heads, 3] = 20, 15
+        x[:, heads + kv_heads:] = c.qkv.reshape(rows, -1, d)[:, heads + kv_heads:]
+        c.qkv[:] = x.reshape(rows, -1)
+        c.forward()
+        torch.cuda.synchronize()
+        see = range(place, rows) if causal else range(rows)
+        want = x[place, heads + kv_heads:].repeat_interleave(heads // kv_heads, 0).reshape(-1)
+        assert torch.equal(c.O[see.start:], want.expand(len(see), -1)), (place, dtype)
+        assert (c.lse[:, see.start:] - 300).abs().max() <= 300 * FP32, place
+        assert torch.isfinite(c.O.float()).all() and (c.lse[:, :see.start] < 10).all()
