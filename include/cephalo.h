@@ -347,7 +347,8 @@ int cephalo_op_attention_bwd(const cephalo_layer_desc* desc, const void* qkv, co
  * length, 0 and 1 too.  No sample's values reach another's results, not-a-numbers and infinities included.  Rows that belong
  * to no sample are neither read nor written, and neither are columns past a row's width.  Inside a sample a row that the causal
  * mask hides has a weight of zero, which in BF16 mode does not silence an infinity or a not-a-number: it can reach the rows
- * less than 128 away.  In F32 mode hidden rows are left out. */
+ * less than 128 away.  In F32 mode hidden rows are left out.
+ * The forward holds for any scores that are finite in 32 bits, times log2(e) too. */
 typedef struct cephalo_packed_desc {
   int32_t heads, kv_heads;   /* heads is a multiple of kv_heads */
   int32_t head_dim;          /* up to 128, in BF16 mode a multiple of 8 */

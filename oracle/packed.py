@@ -11,7 +11,9 @@ def _softmax_parts(q, k, scale, causal):
         n = len(q)
         z = np.where(np.arange(n)[None, :] <= np.arange(n)[:, None], z, -np.inf)
     m = z.max(axis=1, keepdims=True)
-    return z, (m + np.log(np.exp(z - m).sum(axis=1, keepdims=True)))[:, 0]
+    w = np.exp(z - m)
+    total = w.sum(axis=1, keepdims=True)
+    return z, (m + np.log(total))[:, 0], w / total      # (from z - m: at scores of 1e16 a sum of two is lost in lse)
 
 
 def attention_fwd(qkv, starts, heads, kv_heads, d, causal, scale=None):
@@ -26,8 +28,7 @@ def attention_fwd(qkv, starts, heads, kv_heads, d, causal, scale=None):
         for a in range(heads):
             g = a * kv_heads // heads
             q, k, v = x[lo:hi, a], x[lo:hi, heads + g], x[lo:hi, heads + kv_heads + g]
-            z, lse[a, lo:hi] = _softmax_parts(q, k, scale, causal)
-            P = np.exp(z - lse[a, lo:hi, None])
+            _, lse[a, lo:hi], P = _softmax_parts(q, k, scale, causal)
             O[lo:hi, a], mag[lo:hi, a] = P @ v, P @ np.abs(v)
     return O.reshape(len(qkv), -1), lse, mag.reshape(len(qkv), -1)
 
@@ -47,7 +48,7 @@ def attention_bwd(qkv, O, dO, lse, starts, heads, kv_heads, d, causal, scale=Non
             g = a * kv_heads // heads
             ik, iv = heads + g, heads + kv_heads + g
             q, k, v = x[lo:hi, a], x[lo:hi, ik], x[lo:hi, iv]
-            z, _ = _softmax_parts(q, k, scale, causal)
+            z, _, _ = _softmax_parts(q, k, scale, causal)
             P = np.exp(z - lse[a, lo:hi, None])
             D = (do[lo:hi, a] * o[lo:hi, a]).sum(axis=1, keepdims=True)
             dS = P * (do[lo:hi, a] @ v.T - D)

@@ -44,6 +44,24 @@ __device__ __forceinline__ float halves_max(float v) {      // of lanes l and l 
   const unsigned low = r[0], high = r[1];                // (values of their own: a bit cast of a vector's element takes the vector's first)
   return fmaxf(__builtin_bit_cast(float, low), __builtin_bit_cast(float, high));
 }
+// The weights of a row are exp2(s c2 - m), m its largest s c2 so far, rounded: in one instruction, whose own product is not rounded, so that all of a row's weights
+// carry a factor of 2 to the power of m's rounding; their sum and lse carry it too.  From kFar on, where the factor would come to leave 32 bits, rounded products
+// that differ at all differ by 32 or more: only those equal to the largest count.  There the scores become the exponents, 0 or -infinity, as soon as
+// their maximum mx is known, and m is left out of them.
+constexpr float kFar = 0x1p29f;
+__device__ __forceinline__ void far_scores(f32x16 (&s)[2], float m_run, float mx, float c2) {
+#pragma clang fp contract(off)
+  const float m = fmaxf(m_run, mx);
+  if (__any(fabsf(m) >= kFar)) {
+    const bool far = fabsf(m) >= kFar && m != -INFINITY;
+#pragma unroll
+    for (int e = 0; e < 32; ++e) {
+      const float z = s[e >> 4][e & 15] * c2;
+      s[e >> 4][e & 15] = !far ? s[e >> 4][e & 15] : z < m ? -INFINITY : z - m;
+      asm volatile("" : "+v"(s[e >> 4][e & 15]));          // (one after the other: side by side they spill)
+    }
+  }
+}
 // S^T of the 64 keys of the first stage and a wavefront's 32 queries
 template <int D>
 __device__ __forceinline__ void fwd_scores(const FragAddr<D>& at, const bf16x8 (&qf)[D / 16], f32x16 (&s)[2]) {
@@ -101,7 +119,7 @@ __device__ __forceinline__ void fwd_step(const FragAddr<D>& at, const bf16x8 (&q
 #pragma unroll
       for (int e = 0; e < 16; ++e) o[dt][e] *= alpha;
   }
-  const float neg_m = (m_run == -INFINITY) ? 0.f : -m_run;
+  const float neg_m = fabsf(m_run) < kFar ? -m_run : 0.f;      // (0 for a row without a maximum, too)
   float psum = 0.f, m_next = -INFINITY;
   auto prob = [&](int e) {
     const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e >> 4][e & 15], c2, neg_m));
@@ -140,7 +158,10 @@ __device__ __forceinline__ void fwd_step(const FragAddr<D>& at, const bf16x8 (&q
     __builtin_amdgcn_sched_barrier(0);
   });
   l_run += psum;
-  if (NEXT) mx = halves_max(m_next) * c2;                // scores enter the exponent as s * c2 (c2 > 0)
+  if (NEXT) {
+    mx = halves_max(m_next) * c2;                        // scores enter the exponent as s * c2 (c2 > 0)
+    far_scores(nx, m_run, mx, c2);
+  }
 }
 
 // A block has 32 QW queries, 32 a wavefront, and KG groups of wavefronts that take every KG-th tile of the keys, in two stages of their own; the groups'
@@ -248,6 +269,7 @@ packed_fwd_kernel(PackedArgs p, PackedOrder order, const bf16* __restrict__ qkv,
 #pragma unroll
     for (int i = 0; i < 32; ++i) mx = fmaxf(mx, s0[i >> 4][i & 15]);
     mx = halves_max(mx) * c2;
+    far_scores(s0, m_run, mx, c2);
   }
   __syncthreads();                                       // (every wavefront has its scores of tile 0: the keys of tile 2 take its place)
   int i = 0;

@@ -456,3 +456,59 @@ def test_the_largest_score_in_any_place_of_a_tile(dtype, heads, kv_heads, d, row
         assert torch.equal(c.O[see.start:], want.expand(len(see), -1)), (place, dtype)
         assert (c.lse[:, see.start:] - 300).abs().max() <= 300 * FP32, place
         assert torch.isfinite(c.O.float()).all() and (c.lse[:, :see.start] < 10).all()
+
+
+# ---- scores far from zero -----------------------------------------------------------------------------------------------------
+
+# Whole numbers: every product and every partial sum below 2^24 is exact, so the scores are what the definition says and rows have ties.  What is left of the error: the
+# scale times log2(e) is off by 2^-23 of itself, which counts on differences of scores that matter (below 64 in the exponent), and lse is rounded three times.
+def _whole(dtype, heads, kv_heads, d, causal, lengths, scale, most=3, seed=0):
+    c = Packed(dtype, heads, kv_heads, d, causal, lengths, scale=scale, seed=seed)
+    c.scale = float(np.float32(scale))
+    rng = np.random.default_rng(seed)
+    c.qkv[:, :(heads + kv_heads) * d] = torch.from_numpy(rng.integers(-most, most + 1, (c.rows, (heads + kv_heads) * d))).to(TORCH[dtype]).cuda()
+    return c
+
+
+def _check_forward(c):
+    c.forward()
+    torch.cuda.synchronize()
+    O, lse, mag = opacked.attention_fwd(c.host(c.qkv, c.width), c.starts, c.heads, c.kv_heads, c.d, c.causal, c.scale)
+    _within("O", c.host(c.O, c.o_width), O, HALF[c.dtype] * (np.abs(O) + mag) + FP32 * mag)
+    _within("lse", c.lse.double().cpu().numpy(), lse, FP32 * (1 + np.abs(lse)))
+
+
+@pytest.mark.parametrize("dtype,heads,kv_heads,d,lengths", [("bf16", 4, 2, 64, [333, 100]), ("bf16", 4, 2, 128, [333, 100]), ("bf16", 4, 2, 24, [333, 100]), ("bf16", 20, 5, 64, FULL),
+                                                            ("bf16", 16, 4, 128, FULL), ("f32", 4, 2, 64, [333, 100]), ("f32", 2, 1, 100, [200])])
+@pytest.mark.parametrize("scale", [1e3, 1e6, 3e7, 1e9, 1e20, 1e30])
+def test_the_forward_at_any_finite_scores(dtype, heads, kv_heads, d, lengths, scale):
+    """Rows where the keys of the largest score share the weight, exactly."""
+    for causal in (True, False):
+        _check_forward(_whole(dtype, heads, kv_heads, d, causal, lengths, scale))
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 64), ("bf16", 128), ("f32", 64)])
+def test_the_forward_of_large_queries_and_keys(dtype, d):
+    """The default scale, scores up to 1e30."""
+    for size in (2.0 ** 12, 2.0 ** 20, 2.0 ** 45):
+        c = _whole(dtype, 4, 2, d, True, [333, 100], 0.0)
+        c.scale = 1 / math.sqrt(d)
+        c.qkv[:, :(4 + 2) * d] *= size
+        _check_forward(c)
+
+
+@pytest.mark.parametrize("dtype,heads,kv_heads,d", [("bf16", 4, 2, 64), ("bf16", 40, 4, 64), ("bf16", 4, 2, 128), ("bf16", 16, 4, 128), ("f32", 4, 2, 64)])
+@pytest.mark.parametrize("offset,scale", [(0x58B902, 2.0), (1 << 23, 2.0), (-(1 << 23), 2.0), (0x5C5D00, 0.25), (0x58B902, 64.0), (-0x58B902, 64.0)])
+def test_weights_of_scores_that_lie_close_together_far_from_zero(dtype, heads, kv_heads, d, offset, scale):
+    """Scores of offset + small whole numbers that rise along the keys (causal rows raise their maximum on the way), weights of more than one key in a row."""
+    c = _whole(dtype, heads, kv_heads, d, True, [700, 90] if heads < 16 else FULL, scale, most=1)
+    n, sign = heads + kv_heads, 1 if offset > 0 else -1
+    x = torch.zeros(c.rows, n, d, dtype=TORCH[dtype])
+    digits = [abs(offset) >> 16, abs(offset) >> 8 & 255, abs(offset) & 255]
+    for j, v in enumerate(digits):                         # offset = sum of digit * 256^j: 256 * (digit * 256), 16 * (digit * 16), 1 * digit
+        x[:, :heads, j], x[:, heads:, j] = (256, 16, 1)[j], sign * v * (256, 16, 1)[j]
+    x[:, :heads, 3] = 1
+    rng = np.random.default_rng(5)
+    x[:, heads:, 3] = torch.from_numpy(np.minimum(np.arange(c.rows) // 8, 100)[:, None] + rng.integers(-3, 4, (c.rows, kv_heads))).to(TORCH[dtype])
+    c.qkv[:, :n * d] = x.reshape(c.rows, n * d).cuda()
+    _check_forward(c)
