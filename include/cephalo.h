@@ -371,7 +371,9 @@ int cephalo_packed_plan(cephalo_packed_desc* desc, int32_t samples, const int32_
 
 /* Forward: O [tokens, o_pitch] and lse [heads, tokens] fp32, the log-sum-exp of each query row's scaled, masked scores.
  * Backward: dqkv [tokens, qkv_pitch] from dO and what the forward wrote; the sums over the query heads that share a key head are formed
- * in 32 bits, in an order that the list fixes: the same call gives the same bits.  (The list divides the work by all samples of
+ * in 32 bits, in an order that the list fixes: the same call gives the same bits.  The weights are formed again from lse, in 32 bits: each
+ * carries a factor of up to exp((head_dim + 8) 2^-24 s), s the larger of |lse| and scale sum |q| |k| of its row (head_dim 64: 1 % at s = 2300), so that with scores of a
+ * million and more, which the forward holds, the gradients mean nothing.  (The list divides the work by all samples of
  * the batch, so a sample's last bits go by its neighbours' lengths.)  workspace: device,
  * cephalo_op_attention_packed_bwd_workspace(desc) bytes (0: a desc that the calls refuse); no two calls that overlap in time may
  * share it.  plan, qkv, O, dO, lse, dqkv: device, 16-byte aligned.  What a call writes overlaps nothing that it reads. */

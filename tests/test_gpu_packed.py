@@ -512,3 +512,42 @@ def test_weights_of_scores_that_lie_close_together_far_from_zero(dtype, heads, k
     x[:, heads:, 3] = torch.from_numpy(np.minimum(np.arange(c.rows) // 8, 100)[:, None] + rng.integers(-3, 4, (c.rows, kv_heads))).to(TORCH[dtype])
     c.qkv[:, :n * d] = x.reshape(c.rows, n * d).cuda()
     _check_forward(c)
+
+
+def _check_sharp(c):
+    """Of forward and backward at large scores: every weight may carry the factor exp(w), w = (d + 8) 2^-24 s, s the larger of |lse| and the scale times sum |q| |k|.  (A score is a sum of d
+    terms and at most four more, -lse / scale and the roundings of scale log2(e) and of lse log2(e) among them, each rounded to 2^-24 of at most 2 s.)  What lies below 2^-126 may count as zero: a weight, a dS, one of n products or of their sums, each times what follows it."""
+    x, half = c.host(c.qkv, c.width), HALF[c.dtype]
+    c.forward(); c.backward()
+    torch.cuda.synchronize()
+    O, lse, mag = opacked.attention_fwd(x, c.starts, c.heads, c.kv_heads, c.d, c.causal, c.scale)
+    r = np.abs(x).reshape(c.rows, c.heads + 2 * c.kv_heads, c.d)
+    s = max(np.abs(lse).max(), c.scale * max((r[:, a] @ r[:, c.heads + a * c.kv_heads // c.heads].T).max() for a in range(c.heads)))
+    w = math.expm1((c.d + 8) * 2.0 ** -24 * s)
+    dO, X = c.host(c.dO, c.o_width), np.abs(x).max()
+    dP = 2 * c.d * np.abs(dO).max() * X
+    zero = 2 * 2.0 ** -126 * c.rows * (c.heads // c.kv_heads)
+    _within("O", c.host(c.O, c.o_width), O, half * (np.abs(O) + mag) + (FP32 + 2 * w) * mag + zero * (X + 1))
+    got = c.lse.double().cpu().numpy()
+    _within("lse", got, lse, FP32 + w + 2.0 ** -22 * s)
+    grad, weighted, parts = opacked.attention_bwd(x, c.host(c.O, c.o_width), dO, got, c.starts, c.heads, c.kv_heads, c.d, c.causal, c.scale)
+    zero *= np.abs(dO).max() + 1 + c.scale * (dP * X + X + 1)
+    _within("dqkv", c.host(c.dqkv, c.width), grad, half * (np.abs(grad) + weighted) + (FP32 + 2 * w) * parts + zero)
+    return zero / np.abs(grad).max(), w
+
+
+@pytest.mark.parametrize("dtype,heads,kv_heads,d,lengths", [("bf16", 4, 2, 32, [333, 100]), ("bf16", 4, 2, 64, [333, 100]), ("bf16", 4, 2, 128, [333, 100]), ("bf16", 40, 8, 64, FULLER),
+                                                            ("bf16", 32, 8, 128, FULL), ("f32", 4, 2, 64, [333, 100]), ("f32", 4, 2, 100, [333, 100])])
+@pytest.mark.parametrize("scale", [1.0, 16.0, 128.0])
+def test_gradients_at_large_scores_keep_the_stated_accuracy(dtype, heads, kv_heads, d, lengths, scale):
+    for causal in (True, False):
+        _check_sharp(Packed(dtype, heads, kv_heads, d, causal, lengths, scale=scale))
+
+
+@pytest.mark.parametrize("dtype,heads,kv_heads,d,lengths", [("bf16", 4, 2, 32, [333, 100]), ("bf16", 4, 2, 64, [333, 100]), ("bf16", 4, 2, 128, [333, 100]), ("bf16", 40, 8, 64, FULLER),
+                                                            ("bf16", 32, 8, 128, FULL), ("f32", 4, 2, 64, [333, 100]), ("f32", 4, 2, 100, [333, 100])])
+@pytest.mark.parametrize("scale,std", [(float(np.float32(1e30)), 1e-15), (float(np.float32(1e-30)), 1e15), (1e6, 1e-3)])
+def test_both_ends_of_the_scale_with_ordinary_scores(dtype, heads, kv_heads, d, lengths, scale, std):
+    """Queries, keys and values of a size that brings the scores back to ordinary ones."""
+    zero, w = _check_sharp(Packed(dtype, heads, kv_heads, d, True, lengths, scale=float(np.float32(scale)), std=std))
+    assert zero < 1e-4 and w < 1e-2
