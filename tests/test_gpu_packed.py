@@ -551,3 +551,76 @@ def test_both_ends_of_the_scale_with_ordinary_scores(dtype, heads, kv_heads, d, 
     """Queries, keys and values of a size that brings the scores back to ordinary ones."""
     zero, w = _check_sharp(Packed(dtype, heads, kv_heads, d, True, lengths, scale=float(np.float32(scale)), std=std))
     assert zero < 1e-4 and w < 1e-2
+
+
+# ---- forms that the cases above do not reach ----------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("heads,kv_heads,d,lengths", [(4, 2, 72, LENGTHS[2]), (4, 2, 80, LENGTHS[3]), (4, 4, 96, LENGTHS[4]), (5, 1, 90, LENGTHS[5]), (4, 2, 65, LENGTHS[1]), (2, 1, 80, [1]),
+                                                      (8, 1, 80, [700, 3, 260]), (8, 1, 66, [700, 3, 260]), (16, 4, 80, FULL), (16, 4, 90, FULL)])
+def test_f32_heads_of_65_to_96(heads, kv_heads, d, lengths, causal):
+    """The width between: eight wavefronts a block, places of the workspace 128 wide."""
+    print("packed f32", heads, kv_heads, d, lengths, causal, flush=True)
+    c = Packed("f32", heads, kv_heads, d, causal, lengths, before=1, behind=3, gap=5 if d % 2 else 4, seed=d)
+    assert kv_heads > 1 or max(lengths) < 700 or c.desc.joins > 0
+    _check(c)
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("dtype,heads,d,dims,rows", [("bf16", 40, 128, [32, 48, 48], 3301), ("f32", 25, 64, [22, 22, 20], 5301)])
+def test_rotary_results_that_go_past_the_caches(dtype, heads, d, dims, rows, in_place):
+    """Above 32 MiB."""
+    assert rows * heads * d * (2 if dtype == "bf16" else 4) > 32 << 20
+    _rotary(dtype, heads, d, dims, rows, in_place, gap=16, in_place=in_place)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_dropout_results_that_go_past_the_caches(dtype):
+    n, p, seed, first = (1 << 24) + 6149, 0.3, 12345, 64
+    g = torch.Generator(device="cuda").manual_seed(1)
+    branch = torch.randn(n, generator=g, device="cuda").to(TORCH[dtype])
+    resid, dy = (torch.randn(n, generator=g, device="cuda") for _ in range(2))
+    out, dbranch = torch.full((n + 8,), MARK, device="cuda"), torch.full((n + 8,), MARK, dtype=TORCH[dtype], device="cuda")
+    assert out.numel() * 4 > 32 << 20 and dbranch.numel() * dbranch.element_size() > 32 << 20
+    C.cephalo_op_dropout_add(LIB[dtype], branch, resid, out, n, p, seed, first)
+    C.cephalo_op_dropout_bwd(LIB[dtype], dy, dbranch, n, p, seed, first)
+    torch.cuda.synchronize()
+    factor = torch.from_numpy(opacked.dropout_factors(n, p, seed, first)).cuda()
+    for got, want, bound in ((out, resid + factor * branch.double(), 2.0 ** -24 * ((resid + factor * branch.double()).abs() + 2 * (factor * branch.double()).abs())),
+                             (dbranch, factor * dy.double(), (HALF[dtype] + 2.0 ** -23) * (factor * dy.double()).abs())):
+        assert bool(((got[:n].double() - want).abs() <= bound * 1.01).all()) and bool((got[n:] == MARK).all())
+    assert bool((out[:n][factor == 0] == resid[factor == 0]).all()) and bool((dbranch[:n][factor == 0] == 0).all())
+    out[:n] = resid
+    C.cephalo_op_dropout_add(LIB[dtype], branch, out, out, n, p, seed, first)
+    again = torch.empty(n, device="cuda")
+    C.cephalo_op_dropout_add(LIB[dtype], branch, resid, again, n, p, seed, first)
+    torch.cuda.synchronize()
+    assert torch.equal(out[:n], again)
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 64), ("bf16", 128), ("bf16", 24), ("f32", 64), ("f32", 80), ("f32", 100)])
+@pytest.mark.parametrize("causal", [True, False])
+def test_a_list_of_other_samples_writes_nothing_but_the_samples_that_fit(dtype, d, causal):
+    """A longer set's list, with joins: the sample that both sets begin with is done, forward and backward, and no other row is written, neither behind the buffers' rows nor in them."""
+    heads, kv_heads, behind = 16, 1, 700
+    big, small = (Packed(dtype, heads, kv_heads, d, causal, [300, n], seed=1) for n in (500, 60))
+    c = Packed(dtype, heads, kv_heads, d, causal, [300, 60], behind=behind, seed=1)
+    c.desc, c.plan = small.desc, big.plan                 # 360 rows
+    for field in ("tiles", "key_items", "joins", "slots", "plan_bytes"):
+        setattr(c.desc, field, getattr(big.desc, field))
+    assert c.desc.joins > 0 and c.desc.tokens == 360 and c.rows == 360 + behind
+    c.lse = torch.full((heads * 360 + 4096,), MARK, device="cuda")
+    need = C.cephalo_op_attention_packed_bwd_workspace(c.desc)
+    c.workspace = torch.full((need + 65536,), 0xAB, dtype=torch.uint8, device="cuda")
+    c.forward(); c.backward()
+    torch.cuda.synchronize()
+    assert bool((c.O[300:] == MARK).all()) and bool((c.dqkv[300:] == MARK).all()) and bool((c.workspace[need:] == 0xAB).all())
+    lse = c.lse[:heads * 360].reshape(heads, 360)
+    assert bool((lse[:, 300:] == MARK).all()) and bool((c.lse[heads * 360:] == MARK).all())
+    x, half = c.host(c.qkv, c.width)[:300], HALF[dtype]
+    O, want, mag = opacked.attention_fwd(x, [0, 300], heads, kv_heads, d, causal)
+    _within("O", c.host(c.O, c.o_width)[:300], O, half * (np.abs(O) + mag) + FP32 * mag)
+    got = lse[:, :300].double().cpu().numpy()
+    _within("lse", got, want, FP32 * (1 + np.abs(want)))
+    grad, weighted, parts = opacked.attention_bwd(x, c.host(c.O, c.o_width)[:300], c.host(c.dO, c.o_width)[:300], got, [0, 300], heads, kv_heads, d, causal)
+    _within("dqkv", c.host(c.dqkv, c.width)[:300], grad, half * (np.abs(grad) + weighted) + FP32 * parts)
