@@ -365,7 +365,8 @@ typedef struct cephalo_packed_desc {
  * (not decreasing, inside [0, tokens]) is host memory, and so is `plan`, at least cephalo_packed_plan_bytes(samples, tokens)
  * bytes; the caller copies its first desc->plan_bytes bytes to the device, where the calls below take it.  Fills the desc's last fields.
  * The list holds how the work is divided (128 queries of a sample at a time; 128 keys and all or some of the queries that see them), so it goes
- * with the desc that it was made for. */
+ * with the desc that it was made for.  The calls refuse what would pass the 2^32 threads of a launch: about 2^24 pairs of a head and 128 rows of a sample (or
+ * what it has below that), in F32 mode 2^20, with a head_dim above 96 2^21. */
 size_t cephalo_packed_plan_bytes(int32_t samples, int64_t tokens);
 int cephalo_packed_plan(cephalo_packed_desc* desc, int32_t samples, const int32_t* starts, void* plan, size_t plan_bytes);
 

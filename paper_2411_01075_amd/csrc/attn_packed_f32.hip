@@ -11,7 +11,7 @@
 namespace cephalo {
 namespace {
 
-template <int P> constexpr int kW = P <= 6 ? 8 : 4;      // wavefronts of a block
+template <int P> constexpr int kW = packed_f32_waves(P);      // wavefronts of a block
 
 // block l: an eighth of an entry (the eighths of an entry follow one another) and a head
 __device__ __forceinline__ int packed_eighth(const PackedOrder& order, int l, int* place) {
@@ -279,6 +279,7 @@ int launch_attn_packed_bwd_f32(const PackedArgs& a, int causal, const float* qkv
   } else {
 #define CALL(P, V)                                                                                                       \
   packed_f32_dq_kernel<P, V><<<grid, 64 * kW<P>, 0, s>>>(a, order, causal, qkv, O, dO, lse, dvec, dqkv);                 \
+  CEPHALO_CHECK_LAUNCH("attention_packed_dq");                                                                           \
   packed_f32_dkv_kernel<P, V><<<key_grid, 64 * kW<P>, 0, s>>>(a, by_keys, causal, qkv, dO, lse, dvec, dqkv);
     PACKED_F32_FORMS(CALL)
 #undef CALL

@@ -40,9 +40,10 @@ int check_planned(const char* who, const cephalo_packed_desc* d) {
   if (d->samples <= 0 || d->tiles < 0 || d->longest < 0 || d->longest > d->tokens) return fail(CEPHALO_EINVAL, "%s: cephalo_packed_plan has not filled this desc", who);
   if (d->dtype == CEPHALO_BF16 && ((int64_t)d->longest + kPackedTile) * std::max(d->qkv_pitch, d->o_pitch) * 2 >= kRows)
     return fail(CEPHALO_EUNSUPPORTED, "%s: a sample of %d rows exceeds the 2 GiB a buffer offset reaches", who, d->longest);
-  if (((int64_t)d->heads + 7) * std::max(d->tiles, d->key_items) * 8 >= kRows) return fail(CEPHALO_EUNSUPPORTED, "%s: %d heads of %d tiles are too many blocks", who, d->heads, d->tiles);
   if (d->key_items < d->tiles || d->joins < 0 || d->joins > d->tiles || d->slots < 0 || d->slots > d->key_items)
     return fail(CEPHALO_EINVAL, "%s: cephalo_packed_plan has not filled this desc", who);
+  if (packed_threads(d->dtype == CEPHALO_F32, d->tiles, d->key_items, d->heads, d->kv_heads, d->head_dim) >= (int64_t)1 << 32)
+    return fail(CEPHALO_EUNSUPPORTED, "%s: %d heads over %d tiles of 128 rows pass the 2^32 threads of a launch", who, d->heads, d->tiles);
   return CEPHALO_OK;
 }
 size_t part_bytes(const cephalo_packed_desc* d) { return (size_t)d->slots * d->kv_heads * packed_part_floats(d->head_dim) * sizeof(float); }

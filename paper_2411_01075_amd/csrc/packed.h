@@ -41,11 +41,22 @@ __host__ __device__ inline int walk_steps(int causal, int rows, int tile) { retu
 // of the heads, so that the heads that share keys (and the tiles of a head) find them in one L2.  Where an XCD would get half as much again as an
 // equal share (5 heads, 12) the blocks go as they are dealt.
 struct PackedOrder { int units, by_xcd; };
-inline unsigned packed_grid(int entries, int units, PackedOrder* order) {
+inline int64_t packed_blocks(int entries, int units, PackedOrder* order) {
   const int64_t per = (units + 7) / 8;
   const bool by_xcd = 2 * 8 * per <= 3 * (int64_t)units;
   *order = {units, by_xcd};
-  return (unsigned)(by_xcd ? 8 * per * entries : (int64_t)units * entries);
+  return by_xcd ? 8 * per * entries : (int64_t)units * entries;
+}
+inline unsigned packed_grid(int entries, int units, PackedOrder* order) { return (unsigned)packed_blocks(entries, units, order); }
+// Wavefronts of an fp32 block, by its head's pieces of 16 columns; an fp32 block has an eighth of an entry's rows.
+constexpr int packed_f32_waves(int pieces) { return pieces <= 6 ? 8 : 4; }
+// The threads of the largest launch (of its first dimension) that a call makes: a launch takes fewer than 2^32.
+inline int64_t packed_threads(int f32, int tiles, int key_items, int heads, int kv_heads, int d) {
+  PackedOrder order;
+  const int64_t queries = packed_blocks(tiles, heads, &order), keys = packed_blocks(key_items, kv_heads, &order);
+  if (f32) return (queries > keys ? queries : keys) * 8 * 64 * packed_f32_waves((d + 15) / 16);
+  const int64_t by_queries = queries * 256, by_keys = keys * (d <= 64 ? 256 : 512);
+  return by_queries > by_keys ? by_queries : by_keys;
 }
 __device__ __forceinline__ bool packed_block(const PackedOrder& o, int l, int* entry, int* unit) {
   int e, u;

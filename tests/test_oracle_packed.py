@@ -196,6 +196,19 @@ def test_a_sample_beyond_a_buffer_offset_is_refused_and_many_such_rows_are_not()
     assert fwd(plan=None) == -1 and "null" in C.cephalo_last_error()
 
 
+@pytest.mark.parametrize("dtype,heads,kv_heads,d,most", [(C.F32, 32, 4, 8, 1 << 20), (C.F32, 32, 4, 100, 1 << 21), (C.BF16, 64, 8, 64, 1 << 24), (C.BF16, 64, 64, 8, 1 << 24), (C.BF16, 64, 64, 72, 1 << 23)])
+def test_launches_of_too_many_threads_are_refused_before_any(dtype, heads, kv_heads, d, most):
+    """Samples of one row, a block for each and each head (fp32: eight): `most` such pairs are 2^32 threads."""
+    for samples, ok in ((most // heads - 1, True), (most // heads, False)):
+        desc = _desc(heads, kv_heads, d, True, dtype, samples)
+        C.cephalo_packed_plan(desc, range(samples + 1))
+        assert (desc.tiles, desc.key_items) == (samples, samples)
+        fwd, bwd = _calls(desc)
+        for call in (fwd, bwd):
+            assert call(plan=None) == -1 if ok else call() == -2 and "threads of a launch" in C.cephalo_last_error()
+        assert (binding.lib().cephalo_op_attention_packed_bwd_workspace(ctypes.byref(desc)) > 0) == ok
+
+
 def test_no_samples_no_launch():
     d = _desc()
     C.cephalo_packed_plan(d, [4, 4, 4])
