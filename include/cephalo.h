@@ -389,7 +389,8 @@ int cephalo_op_attention_packed_bwd(const cephalo_packed_desc* desc, const void*
  *   positions[row][k] * base^(-2i / axis_dims[k]),   inverse: by the negative angle (the gradient's way back).
  * positions: device int32 [rows, axes]; axis_dims: HOST [axes], axes 1 to 8.  The angle is formed in 64 bits.  src and dst (device, pitches in elements) may be
  * the same buffer with the same pitch; they must not overlap otherwise.  Queries and keys of the packed projection are neighbours: heads + kv_heads
- * heads in one call.  head_dim: up to 128, a multiple of 8 (BF16) or 4 (F32), and so are the pitches. */
+ * heads in one call.  head_dim: up to 128, a multiple of 8 (BF16) or 4 (F32), and so are the pitches.  One call takes 2^24 - 2 rows whatever their width, more of narrow
+ * ones (up to 2^32 threads of four heads' 16 bytes each). */
 int cephalo_op_rotary_axes(int32_t dtype, const void* src, int64_t src_pitch, void* dst, int64_t dst_pitch, const int32_t* positions, int64_t rows,
                            int32_t axes, const int32_t* axis_dims, int32_t heads, int32_t head_dim, double base, int32_t inverse, void* stream);
 
@@ -398,7 +399,7 @@ int cephalo_op_rotary_axes(int32_t dtype, const void* src, int64_t src_pitch, vo
  * (the gradient of resid is dy itself).  keep_i: 16-bit word first + i of the stream of `seed` is at least round(65536 p); scale = 65536 / (65536 - round(65536 p)).
  * Words 8j .. 8j+7 of a stream are the four results of Philox4x32-10 (Salmon et al., 2011) for counter j and key seed, the low half of each first.  An
  * element's word depends on its place alone: calls on parts of a tensor, each with its own `first`, drop what one call drops.
- *   branch, dbranch  device, n in dtype;  resid, out, dy  device, n fp32; out may be resid
+ *   branch, dbranch  device, n in dtype;  resid, out, dy  device, n fp32; out may be resid;  n below 2^35 - 2048
  *   p                in [0, 1), a multiple of 2^-16 after rounding;  first: a multiple of 8
  *   counter          device, one 64-bit word that is added to `first` when the kernel runs (a multiple of 8: it is rounded down), or NULL.  A captured
  *                    graph draws new words at each replay if the caller advances it between them. */

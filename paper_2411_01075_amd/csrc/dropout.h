@@ -4,6 +4,8 @@
 
 namespace cephalo {
 
+constexpr int kDropoutBlock = 256;
+constexpr int64_t kDropoutMost = (((int64_t)1 << 32) / kDropoutBlock - 1) * kDropoutBlock * 8;      // a thread has 8 elements, a launch fewer than 2^32 threads
 struct DropoutArgs {
   int64_t n;
   uint64_t seed, first;              // first: a multiple of 8

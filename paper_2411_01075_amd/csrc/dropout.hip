@@ -45,9 +45,9 @@ template <typename T, bool STREAM> __device__ __forceinline__ void store8(T* p, 
 
 // ADD: out = resid + dropout(in), fp32;  else out = dropout(in)
 template <typename IN, typename OUT, bool ADD, bool STREAM>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(kDropoutBlock)
 dropout_kernel(DropoutArgs d, const IN* __restrict__ in, const float* resid, OUT* out) {
-  const int64_t group = (int64_t)blockIdx.x * 256 + threadIdx.x, at = group * 8;
+  const int64_t group = (int64_t)blockIdx.x * kDropoutBlock + threadIdx.x, at = group * 8;
   if (at >= d.n) return;
   const uint64_t first = d.first + (d.counter ? *d.counter : 0);
   float x[8], r[8];
@@ -79,13 +79,13 @@ dropout_kernel(DropoutArgs d, const IN* __restrict__ in, const float* resid, OUT
 
 template <typename IN, typename OUT, bool ADD>
 int launch(const DropoutArgs& d, const IN* in, const float* resid, OUT* out, hipStream_t s) {
-  const int64_t blocks = (d.n + 2047) / 2048;
+  const int64_t blocks = (d.n + kDropoutBlock * 8 - 1) / (kDropoutBlock * 8);
   if (blocks == 0) return CEPHALO_OK;
   // Results beyond 32 MiB, which the L2s together do not hold, go past them: 12288 x 2048, bf16 branch, forward 44 -> 41.7 us (6.0 TB/s), backward 28.2 -> 21.3.
   // (Two or four groups of 8 a thread: no difference, and 131 x 257 3.4 and 4.0 us instead of 2.5.)
   const bool stream = d.n * (int64_t)sizeof(OUT) > (int64_t)32 << 20;
   const auto kern = stream ? dropout_kernel<IN, OUT, ADD, true> : dropout_kernel<IN, OUT, ADD, false>;
-  kern<<<(unsigned)blocks, 256, 0, s>>>(d, in, resid, out);
+  kern<<<(unsigned)blocks, kDropoutBlock, 0, s>>>(d, in, resid, out);
   CEPHALO_CHECK_LAUNCH("dropout");
   return CEPHALO_OK;
 }

@@ -204,6 +204,8 @@ extern "C" int cephalo_op_rotary_axes(int32_t dtype, const void* src, int64_t sr
   if (src_pitch < width || dst_pitch < width || src_pitch % vec != 0 || dst_pitch % vec != 0)
     return fail(CEPHALO_EINVAL, "rotary_axes: pitches %lld and %lld must cover %lld columns in multiples of %d", (long long)src_pitch, (long long)dst_pitch, (long long)width, vec);
   if (width >= kRows) return fail(CEPHALO_EUNSUPPORTED, "rotary_axes: rows of %lld columns", (long long)width);
+  if (rows / rotary_split(heads, head_dim, vec).rows >= ((int64_t)1 << 32) / 256 - 1)
+    return fail(CEPHALO_EUNSUPPORTED, "rotary_axes: %lld rows of %d heads pass the 2^32 threads of a launch", (long long)rows, heads);
   RotaryAxes r = {};
   r.src_pitch = src_pitch; r.dst_pitch = dst_pitch; r.heads = heads; r.d = head_dim; r.axes = axes;
   int pair = 0;
@@ -230,7 +232,8 @@ extern "C" int cephalo_op_rotary_axes(int32_t dtype, const void* src, int64_t sr
 namespace {
 int dropout_args(const char* who, int dtype, int64_t n, float p, uint64_t seed, int64_t first, const uint64_t* counter, DropoutArgs* d) {
   if (const int rc = check_dtype(who, dtype); rc != CEPHALO_OK) return rc;
-  if (n < 0 || n > (int64_t)1 << 41) return fail(CEPHALO_EINVAL, "%s: %lld elements", who, (long long)n);
+  if (n < 0) return fail(CEPHALO_EINVAL, "%s: %lld elements", who, (long long)n);
+  if (n >= kDropoutMost) return fail(CEPHALO_EUNSUPPORTED, "%s: %lld elements pass the 2^32 threads of a launch", who, (long long)n);
   if (!(p >= 0.f && p < 1.f)) return fail(CEPHALO_EINVAL, "%s: p %g is not in [0, 1)", who, p);
   const int drop = (int)std::floor((double)p * 65536.0 + 0.5);
   if (drop > 65535) return fail(CEPHALO_EINVAL, "%s: p %g leaves nothing", who, p);

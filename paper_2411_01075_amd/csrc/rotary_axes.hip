@@ -51,18 +51,13 @@ rotary_axes_kernel(RotaryAxes r, const T* __restrict__ src, T* __restrict__ dst,
 
 template <typename T>
 int launch_rotary_axes(const RotaryAxes& r, const T* src, T* dst, const int* positions, int64_t rows, hipStream_t s) {
-  constexpr int HEADS = 4;
-  const int chunks = r.d / Vec<T>::N;
-  int parts = (r.heads + HEADS - 1) / HEADS;
-  if (parts * chunks > 256) parts = 256 / chunks;
-  const int rows_per_block = 256 / (parts * chunks);
-  const int64_t blocks = (rows + rows_per_block - 1) / rows_per_block;
-  if (blocks >= (int64_t)1 << 31) return fail(CEPHALO_EUNSUPPORTED, "rotary_axes: %lld rows", (long long)rows);
+  const RotarySplit split = rotary_split(r.heads, r.d, Vec<T>::N);
+  const int64_t blocks = (rows + split.rows - 1) / split.rows;
   // Results beyond 32 MiB, which the L2s together do not hold, go past them: 16384 rows of 40 heads of 128 (bf16, 335 MB in and out) 61.2 -> 55.8 us, the rate
   // of a copy.
   const bool stream = (int64_t)rows * r.heads * r.d * (int64_t)sizeof(T) > (int64_t)32 << 20;
-  const auto kern = stream ? rotary_axes_kernel<T, HEADS, true> : rotary_axes_kernel<T, HEADS, false>;
-  kern<<<(unsigned)blocks, 256, 0, s>>>(r, src, dst, positions, rows, chunks, parts, rows_per_block);
+  const auto kern = stream ? rotary_axes_kernel<T, kRotaryHeads, true> : rotary_axes_kernel<T, kRotaryHeads, false>;
+  kern<<<(unsigned)blocks, 256, 0, s>>>(r, src, dst, positions, rows, split.chunks, split.parts, split.rows);
   CEPHALO_CHECK_LAUNCH("rotary_axes");
   return CEPHALO_OK;
 }

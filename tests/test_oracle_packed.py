@@ -232,6 +232,18 @@ def test_rotary_refusals():
     assert _rotary(rows=0, src=None, dst=None, positions=None) == 0
 
 
+def test_rotary_and_dropout_launches_of_too_many_threads_are_refused():
+    for kw in (dict(rows=1 << 24, heads=300, d=128, src_pitch=300 * 128, dst_pitch=300 * 128, dims=(128,)), dict(rows=1 << 28, heads=1, d=128, src_pitch=128, dst_pitch=128, dims=(128,)),
+               dict(rows=1 << 62), dict(dtype=C.F32, rows=1 << 27, heads=8, src_pitch=512, dst_pitch=512)):
+        assert _rotary(**kw) == -2 and "threads of a launch" in C.cephalo_last_error(), kw
+    for kw in (dict(rows=(1 << 24) - 2, heads=300, d=128, src_pitch=300 * 128, dst_pitch=300 * 128, dims=(128,)), dict(rows=(1 << 28) - 32, heads=1, d=128, src_pitch=128, dst_pitch=128, dims=(128,))):
+        assert _rotary(positions=None, **kw) == -1 and "null" in C.cephalo_last_error(), kw
+    L = binding.lib()
+    for n, code in ((2 ** 35 - 2048, -2), (2 ** 41, -2), (2 ** 62, -2), (2 ** 35 - 2049, -1)):
+        assert L.cephalo_op_dropout_add(C.BF16, None, FAKE, FAKE, n, 0.1, 1, 0, None, None) == code
+        assert L.cephalo_op_dropout_bwd(C.F32, FAKE, None, n, 0.1, 1, 0, None, None) == code
+
+
 def test_dropout_refusals():
     L = binding.lib()
     add = lambda dtype=C.BF16, branch=FAKE, resid=FAKE, out=FAKE, n=8, p=0.1, first=0, counter=None: L.cephalo_op_dropout_add(dtype, branch, resid, out, n, p, 1, first, counter, None)      # noqa: E731
