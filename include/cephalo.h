@@ -344,7 +344,7 @@ int cephalo_op_attention_bwd(const cephalo_layer_desc* desc, const void* qkv, co
  * queries, then `kv_heads` keys, then `kv_heads` values of head_dim columns; query head a reads key head
  * a / (heads / kv_heads), so that kv_heads = heads is the form above and kv_heads = 1 shares one key head.
  * Attention stays inside a sample: query row q of it sees its rows t <= q (causal) or all of them.  Samples may have any
- * length, 0 and 1 too.  No sample's values reach another's results, not-a-numbers and infinities included.  Rows that belong
+ * length up to 2^30, 0 and 1 too; in BF16 mode a sample's rows and 128 more, each of the longer pitch, stay below 2 GiB.  No sample's values reach another's results, not-a-numbers and infinities included.  Rows that belong
  * to no sample are neither read nor written, and neither are columns past a row's width.  Inside a sample a row that the causal
  * mask hides has a weight of zero, which in BF16 mode does not silence an infinity or a not-a-number: it can reach the rows
  * less than 128 away.  In F32 mode hidden rows are left out.

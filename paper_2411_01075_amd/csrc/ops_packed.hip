@@ -9,6 +9,7 @@ using namespace cephalo;
 
 namespace {
 constexpr int64_t kRows = (int64_t)1 << 31;      // rows are counted in 32 bits
+constexpr int kLongest = 1 << 30;                // of a sample, whose rows are added to and rounded up in them
 
 int check_dtype(const char* who, int dtype) {
   if (dtype != CEPHALO_F32 && dtype != CEPHALO_BF16) return fail(CEPHALO_EINVAL, "%s: unknown dtype %d", who, dtype);
@@ -37,7 +38,7 @@ int check_packed(const char* who, const cephalo_packed_desc* d) {
 // a desc whose work list was made, and what the kernels' index arithmetic holds
 int check_planned(const char* who, const cephalo_packed_desc* d) {
   if (const int rc = check_packed(who, d); rc != CEPHALO_OK) return rc;
-  if (d->samples <= 0 || d->tiles < 0 || d->longest < 0 || d->longest > d->tokens) return fail(CEPHALO_EINVAL, "%s: cephalo_packed_plan has not filled this desc", who);
+  if (d->samples <= 0 || d->tiles < 0 || d->longest < 0 || d->longest > std::min<int64_t>(d->tokens, kLongest)) return fail(CEPHALO_EINVAL, "%s: cephalo_packed_plan has not filled this desc", who);
   if (d->dtype == CEPHALO_BF16 && ((int64_t)d->longest + kPackedTile) * std::max(d->qkv_pitch, d->o_pitch) * 2 >= kRows)
     return fail(CEPHALO_EUNSUPPORTED, "%s: a sample of %d rows exceeds the 2 GiB a buffer offset reaches", who, d->longest);
   if (d->key_items < d->tiles || d->joins < 0 || d->joins > d->tiles || d->slots < 0 || d->slots > d->key_items)
@@ -109,6 +110,7 @@ extern "C" int cephalo_packed_plan(cephalo_packed_desc* d, int32_t samples, cons
     if (starts[i + 1] < starts[i]) return fail(CEPHALO_EINVAL, "packed_plan: sample %d ends before it starts (rows %d, %d)", i, starts[i], starts[i + 1]);
     longest = std::max(longest, starts[i + 1] - starts[i]);
   }
+  if (longest > kLongest) return fail(CEPHALO_EUNSUPPORTED, "packed_plan: a sample of %d rows, %d at most", longest, kLongest);
   PackedTile* list = static_cast<PackedTile*>(plan);
   const int causal = d->causal, group = d->heads / d->kv_heads;
   int tiles = 0;

@@ -209,6 +209,17 @@ def test_launches_of_too_many_threads_are_refused_before_any(dtype, heads, kv_he
         assert (binding.lib().cephalo_op_attention_packed_bwd_workspace(ctypes.byref(desc)) > 0) == ok
 
 
+@pytest.mark.parametrize("rows,code", [(2 ** 30, 0), (2 ** 30 + 1, -2), (2 ** 31 - 64, -2), (2 ** 31 - 63, -2), (2 ** 31 - 1, -2)])
+def test_samples_whose_rows_pass_the_kernels_counters_are_refused(rows, code):
+    """A longer sample's steps would be counted past 2^31."""
+    d, L = _desc(1, 1, 4, False, C.F32, rows), binding.lib()
+    plan = np.empty(L.cephalo_packed_plan_bytes(1, rows) // 4, np.int32)      # (untouched pages take no memory)
+    assert L.cephalo_packed_plan(ctypes.byref(d), 1, (ctypes.c_int32 * 2)(0, rows), plan.ctypes.data, plan.nbytes) == code
+    if code == 0:
+        keys = plan[4 * d.tiles:4 * d.tiles + 8 * d.key_items].reshape(-1, 8)
+        assert (keys[:, 3] >= 0).all() and (keys[:, 4] > keys[:, 3]).all() and keys[:, 4].max() <= (rows + 63) // 64
+
+
 def test_no_samples_no_launch():
     d = _desc()
     C.cephalo_packed_plan(d, [4, 4, 4])
