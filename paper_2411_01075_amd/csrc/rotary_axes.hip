@@ -11,7 +11,7 @@ namespace {
 
 template <typename T, int HEADS, bool STREAM>
 __global__ void __launch_bounds__(256)
-rotary_axes_kernel(RotaryAxes r, const T* __restrict__ src, T* __restrict__ dst, const int* __restrict__ positions, int64_t rows, int chunks, int parts, int rows_per_block) {
+rotary_axes_kernel(RotaryAxes r, const T* src, T* dst, const int* __restrict__ positions, int64_t rows, int chunks, int parts, int rows_per_block) {      // (src may be dst)
   constexpr int V = Vec<T>::N, PAIRS = V / 2;
   const int per_row = chunks * parts, in_block = threadIdx.x / per_row, rest = threadIdx.x % per_row;
   const int64_t row = (int64_t)blockIdx.x * rows_per_block + in_block;
@@ -28,7 +28,7 @@ rotary_axes_kernel(RotaryAxes r, const T* __restrict__ src, T* __restrict__ dst,
     float x[HEADS][V];
 #pragma unroll
     for (int k = 0; k < HEADS; ++k) {
-      const int head = min(head0 + k * parts, r.heads - 1);
+      const int head = head0 + k * parts < r.heads ? head0 + k * parts : head0;      // (of its own heads: another's may be written meanwhile)
       load_vec<T>(src + row * r.src_pitch + head * r.d + c * V, x[k]);
     }
 #pragma unroll
