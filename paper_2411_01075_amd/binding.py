@@ -426,6 +426,16 @@ def _buffer(what, t, dtype, elements, device):
     return t.data_ptr()
 
 
+def _rows(what, t, dtype, rows, width, pitch, device):
+    """The same for `rows` rows of `width` elements that begin `pitch` elements apart: a contiguous tensor, or a view of some columns whose first dimension is the rows."""
+    if t.is_contiguous() or t.dim() < 2 or t.get_device() != device:
+        return _buffer(what, t, dtype, max(rows - 1, 0) * pitch + (width if rows > 0 else 0), device)
+    if t.stride(0) != pitch or t.shape[0] < rows:
+        raise CephaloError("%s: expected %d rows %d elements apart, got %d and %d" % (what, rows, pitch, t.shape[0], t.stride(0)))
+    _buffer(what, t[0], dtype, width, device)
+    return t.data_ptr()
+
+
 def _device():
     return torch.cuda.current_device() if torch.cuda.is_initialized() else -2      # (a host tensor's index is -1)
 
@@ -440,9 +450,9 @@ def cephalo_packed_plan(desc, starts):
 
 
 def _packed_buffers(desc, plan, qkv, O, lse, device):
-    rows, width, dtype = max(desc.tokens - 1, 0), desc.heads * desc.head_dim, desc.dtype
-    of_qkv, of_o = rows * desc.qkv_pitch + width + 2 * desc.kv_heads * desc.head_dim, rows * desc.o_pitch + width
-    return (_buffer("plan", plan, "int32", desc.plan_bytes // 4, device), of_qkv, of_o, _buffer("qkv", qkv, dtype, of_qkv, device), _buffer("O", O, dtype, of_o, device),
+    of_qkv = (desc.dtype, desc.tokens, (desc.heads + 2 * desc.kv_heads) * desc.head_dim, desc.qkv_pitch, device)
+    of_o = (desc.dtype, desc.tokens, desc.heads * desc.head_dim, desc.o_pitch, device)
+    return (_buffer("plan", plan, "int32", desc.plan_bytes // 4, device), of_qkv, of_o, _rows("qkv", qkv, *of_qkv), _rows("O", O, *of_o),
             _buffer("lse", lse, F32, desc.heads * desc.tokens, device))
 
 
@@ -461,15 +471,15 @@ def cephalo_op_attention_packed_bwd_workspace(desc):
 def cephalo_op_attention_packed_bwd(desc, plan, qkv, O, dO, lse, dqkv, workspace, stream=None):
     device = _device()
     plan, of_qkv, of_o, qkv, O, lse = _packed_buffers(desc, plan, qkv, O, lse, device)
-    dO, dqkv = _buffer("dO", dO, desc.dtype, of_o, device), _buffer("dqkv", dqkv, desc.dtype, of_qkv, device)
+    dO, dqkv = _rows("dO", dO, *of_o), _rows("dqkv", dqkv, *of_qkv)
     _check(lib().cephalo_op_attention_packed_bwd(ctypes.byref(desc), plan, qkv, O, dO, lse, dqkv, _buffer("workspace", workspace, None, 0, device), _nbytes(workspace),
                                                  _stream(stream)))
 
 
 def cephalo_op_rotary_axes(dtype, src, src_pitch, dst, dst_pitch, positions, rows, axis_dims, heads, head_dim, base=10000.0, inverse=False, stream=None):
     """axis_dims: the columns of a head that each axis turns (host); positions: int32 [rows, axes]."""
-    device, last, width, axes = _device(), max(rows - 1, 0), heads * head_dim if rows > 0 else 0, len(axis_dims)
-    src, dst = _buffer("src", src, dtype, last * src_pitch + width, device), _buffer("dst", dst, dtype, last * dst_pitch + width, device)
+    device, width, axes = _device(), heads * head_dim, len(axis_dims)
+    src, dst = _rows("src", src, dtype, rows, width, src_pitch, device), _rows("dst", dst, dtype, rows, width, dst_pitch, device)
     _check(lib().cephalo_op_rotary_axes(dtype, src, src_pitch, dst, dst_pitch, _buffer("positions", positions, "int32", rows * axes, device), rows, axes, _ints(axis_dims),
                                         heads, head_dim, base, int(inverse), _stream(stream)))
 

@@ -624,3 +624,48 @@ def test_a_list_of_other_samples_writes_nothing_but_the_samples_that_fit(dtype, 
     _within("lse", got, want, FP32 * (1 + np.abs(want)))
     grad, weighted, parts = opacked.attention_bwd(x, c.host(c.O, c.o_width)[:300], c.host(c.dO, c.o_width)[:300], got, [0, 300], heads, kv_heads, d, causal)
     _within("dqkv", c.host(c.dqkv, c.width)[:300], grad, half * (np.abs(grad) + weighted) + FP32 * parts)
+
+
+# ---- views ------------------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 64), ("bf16", 128), ("f32", 64)])
+def test_attention_on_columns_of_wider_tensors(dtype, d):
+    c, v = (Packed(dtype, 4, 2, d, True, [130, 0, 70, 1], before=3, behind=6) for _ in range(2))
+    c.forward(); c.backward()
+    wide = {n: torch.full((c.rows + 2, getattr(c, n).shape[1] + 48), MARK, dtype=TORCH[dtype], device="cuda") for n in ("qkv", "O", "dO", "dqkv")}
+    part = {n: t[1:-1, 16:-32] for n, t in wide.items()}
+    part["qkv"].copy_(c.qkv); part["dO"].copy_(c.dO)
+    v.desc.qkv_pitch, v.desc.o_pitch = wide["qkv"].stride(0), wide["O"].stride(0)
+    for n in wide:
+        setattr(v, n, part[n].unflatten(1, (-1, d)) if n == "O" else part[n])
+    v.forward(); v.backward()
+    torch.cuda.synchronize()
+    assert torch.equal(part["O"], c.O) and torch.equal(v.lse, c.lse) and torch.equal(part["dqkv"], c.dqkv)
+    for n, t in wide.items():
+        assert bool((t[0] == MARK).all()) and bool((t[-1] == MARK).all()) and bool((t[:, :16] == MARK).all()) and bool((t[:, -32:] == MARK).all()), n
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rotary_on_the_keys_of_a_projection_in_place(dtype):
+    heads, kv_heads, d, rows = 4, 2, 64, 77
+    qkv = torch.randn(rows, (heads + 2 * kv_heads) * d, device="cuda").to(TORCH[dtype])
+    positions = torch.arange(rows, dtype=torch.int32, device="cuda")[:, None].contiguous()
+    keys, before = qkv[:, heads * d:(heads + kv_heads) * d], qkv.clone()
+    want = torch.empty(rows, kv_heads * d, dtype=TORCH[dtype], device="cuda")
+    C.cephalo_op_rotary_axes(LIB[dtype], keys.contiguous(), kv_heads * d, want, kv_heads * d, positions, rows, [64], kv_heads, d)
+    C.cephalo_op_rotary_axes(LIB[dtype], keys, qkv.stride(0), keys, qkv.stride(0), positions, rows, [64], kv_heads, d)
+    torch.cuda.synchronize()
+    assert torch.equal(keys, want)
+    assert torch.equal(qkv[:, :heads * d], before[:, :heads * d]) and torch.equal(qkv[:, (heads + kv_heads) * d:], before[:, (heads + kv_heads) * d:])
+
+
+def test_views_that_do_not_cover_the_rows_are_refused():
+    x = torch.zeros(8, 48, device="cuda")
+    p = torch.zeros(8, 1, dtype=torch.int32, device="cuda")
+    call = lambda src, rows=8, pitch=48: C.cephalo_op_rotary_axes(C.F32, src, pitch, src, pitch, p, rows, [16], 1, 16)      # noqa: E731
+    call(x[:, 16:32]); call(x[:, 32:]); call(x[1:, 32:], rows=7); call(x[:, 16:32], rows=1); call(x[:, 16:32], rows=0)
+    for bad in (lambda: call(x[:, 16:31]), lambda: call(x[:7, 16:32]), lambda: call(x[:, 16:32], pitch=40), lambda: call(x[::2, 16:32], rows=4), lambda: call(x.t()[16:32].t()[:, ::2]),
+                lambda: call(x[:, 16:32].double()), lambda: call(x.cpu()[:, 16:32])):
+        with pytest.raises(C.CephaloError, match="expected"):
+            bad()
+    torch.cuda.synchronize()
