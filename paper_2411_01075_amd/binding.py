@@ -360,6 +360,9 @@ def cephalo_op_linear_wgrad_bias(dtype, dY, X, T, N, K, G, gb, scale, accumulate
 
 
 def _ints(values):
+    for v in values:      # (ctypes would take it modulo 2^32)
+        if not -2 ** 31 <= v < 2 ** 31:
+            raise CephaloError("%d does not fit 32 bits" % v)
     return (_i32 * len(values))(*values)
 
 

@@ -139,6 +139,13 @@ def test_starts_outside_the_rows_are_refused(starts, says):
         C.cephalo_packed_plan(_desc(), starts)
 
 
+@pytest.mark.parametrize("starts", [[0, 2 ** 32 + 5], [2 ** 32, 2 ** 32 + 5], [-2 ** 32, 5], [0, 2 ** 31]])
+def test_starts_that_pass_32_bits_are_refused(starts):
+    """Not taken modulo 2^32, where they would lie inside the rows."""
+    with pytest.raises(C.CephaloError, match="32 bits"):
+        C.cephalo_packed_plan(_desc(), starts)
+
+
 def test_a_list_buffer_that_is_too_small_is_refused():
     d, L = _desc(), binding.lib()
     starts = (ctypes.c_int32 * 3)(0, 500, 1000)
