@@ -69,7 +69,8 @@ bool all_aligned(std::initializer_list<const void*> ptrs) {
 }  // namespace
 
 namespace {
-constexpr int kMostPieces = 1024;      // pieces that a list cuts its keys' walks into, beyond one each
+// Pieces that a list cuts its keys' walks into, beyond one each: fewer than walk / share of each, and the share is at least all the steps over 512.
+constexpr int kMostPieces = 512;
 
 // How many steps of a walk an item takes, and by how many the longest walk may exceed that without any being cut.  A launch lasts as long as its longest block,
 // and a key tile's walk is as long as the queries that see it times the heads that share it, so few keys and long walks leave the chip idle: walks
@@ -132,17 +133,12 @@ extern "C" int cephalo_packed_plan(cephalo_packed_desc* d, int32_t samples, cons
   if (longest_walk > (int64_t)1 << 30) return fail(CEPHALO_EUNSUPPORTED, "packed_plan: %d rows under %d heads of a key head", longest, group);
   const Share share = steps_an_item(d, tiles, steps);
   const bool cut = longest_walk > (int64_t)share.steps + share.slack;
-  int items = 0, joins = 0, slots = 0, spare = kMostPieces;
-  auto pieces_of = [&](const PackedTile& e) {
-    const int64_t walk = (int64_t)walk_steps(causal, e.rows, e.tile) * group;
-    return cut && walk * 4 > (int64_t)share.steps * 5 ? (int)((walk + share.steps - 1) / share.steps) : 1;
-  };
+  int items = 0, joins = 0, slots = 0;
   KeyItem* keys = reinterpret_cast<KeyItem*>(list + tiles);
   for (int i = 0; i < tiles; ++i) {
     const PackedTile& e = list[i];
     const int64_t walk = (int64_t)walk_steps(causal, e.rows, e.tile) * group;
-    const int pieces = std::min(pieces_of(e), spare + 1);
-    spare -= pieces - 1;
+    const int pieces = cut && walk * 4 > (int64_t)share.steps * 5 ? (int)((walk + share.steps - 1) / share.steps) : 1;
     for (int q = 0; q < pieces; ++q)
       keys[items++] = {e.first, e.rows, e.tile, (int)(walk * q / pieces), (int)(walk * (q + 1) / pieces), pieces > 1 ? slots + q : -1, pieces, 0};
     if (pieces > 1) { slots += pieces; ++joins; }

@@ -133,6 +133,22 @@ def test_the_walks_of_the_keys_cover_the_queries_once(heads, kv_heads, d, starts
     assert not joined and used == set(range(desc.slots))
 
 
+@pytest.mark.parametrize("dtype", [C.BF16, C.F32])
+@pytest.mark.parametrize("d", [32, 128])
+def test_the_pieces_of_any_list_have_room(d, dtype):
+    """A list's buffer holds 512 pieces beyond one a tile: no set of samples takes more."""
+    rng, most = np.random.default_rng(d), 0
+    for _ in range(300):
+        kv_heads, group = int(rng.choice([1, 1, 2, 8])), int(rng.choice([1, 4, 16, 64]))
+        lengths = np.exp(rng.uniform(0, rng.uniform(1, 12), int(rng.integers(1, 200)))).astype(int)
+        starts = [0] + np.cumsum(lengths).tolist()
+        desc = C.packed_desc(kv_heads * group, kv_heads, d, bool(rng.integers(2)), dtype, starts[-1])
+        plan = C.cephalo_packed_plan(desc, starts)
+        most = max(most, desc.key_items - desc.tiles)
+        assert desc.key_items - desc.tiles < 512 and plan.numel() * 4 <= binding.lib().cephalo_packed_plan_bytes(len(lengths), desc.tokens)
+    assert most > (64 if dtype == C.BF16 else 4)
+
+
 @pytest.mark.parametrize("starts,says", [([0, 5, 4], "ends before it starts"), ([-1, 5], "from row -1"), ([0, 1001], "to 1001"), ([0], "0 samples")])
 def test_starts_outside_the_rows_are_refused(starts, says):
     with pytest.raises(C.CephaloError, match=says):
