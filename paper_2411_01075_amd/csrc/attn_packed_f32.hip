@@ -3,7 +3,7 @@
 // turn, straight from memory; their results are merged in wavefront order.  Rows past a sample's end are read as zeros.
 //
 // What bounds it is the chain of loads and products of one block of 16, 3 to 5 us: eight wavefronts share it, or four where a head's registers
-// allow no more, and the backward of heads up to 64 is one launch up to 1024 blocks (dK / dV forms rowsum(dO O) itself).  611 tokens, the longest sample 401, 4 heads of 64 over 2,
+// allow no more, and the backward of heads up to 64 is one launch where few blocks run (dK / dV forms rowsum(dO O) itself).  611 tokens, the longest sample 401, 4 heads of 64 over 2,
 // four wavefronts and two launches -> this: forward 23 -> 17 us, backward 53 -> 33 (with its join).
 #include "attn_f32_tile.h"
 #include "packed.h"
@@ -271,7 +271,9 @@ int launch_attn_packed_bwd_f32(const PackedArgs& a, int causal, const float* qkv
   const bool vec = a.d % 4 == 0 && a.ld % 4 == 0 && a.ldo % 4 == 0;
   PackedOrder order, by_keys;
   const unsigned grid = 8 * packed_grid(a.tiles, a.heads, &order), key_grid = 8 * packed_grid(a.key_items, a.kv_heads, &by_keys);
-  if ((int64_t)grid + key_grid <= 1024 && a.d <= 64) {      // (wider heads: the two halves together spill)
+  // One launch, us in two and in one, by blocks: 448: 39 and 27; 864: 93 and 84; 1376: 248 and 226; 1536: 95 and 100; 4096: 434 and 459.  (Wider heads: the two
+  // halves together spill.)
+  if ((int64_t)grid + key_grid <= 1408 && a.d <= 64) {
 #define CALL(P, V) packed_f32_bwd_kernel<P, V><<<grid + key_grid, 64 * kW<P>, 0, s>>>(a, by_keys, order, (int)key_grid, causal, qkv, O, dO, lse, dqkv);
     if (vec) { if (a.d <= 32) { CALL(2, true) } else { CALL(4, true) } }
     else { if (a.d <= 32) { CALL(2, false) } else { CALL(4, false) } }

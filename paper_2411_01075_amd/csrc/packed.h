@@ -28,9 +28,10 @@ __host__ __device__ inline int packed_width(int d) { return d <= 32 ? 32 : d <= 
 inline size_t packed_part_floats(int d) { return 2 * (size_t)kPackedTile * packed_width(d); }
 
 // Whether the bf16 backward is one launch: where its two halves, one after the other, would leave compute units idle.  Us in two and in one, by tiles times
-// (heads + key heads).  Heads of 64: 48: 26 and 16; 320: 68 and 53; 512: 28 and 21; 640: 36 and 36; 768: 41 and 35; 1024: 32 and 32.  Heads of 128: 128: 54
-// and 37; 320: 83 and 63; 512: 112 and 91; 640: 308 and 279; 1024: 88 and 101; 1280: 526 and 548.  (Two: dQ blocks of 128 queries.)
-inline bool packed_one_launch(int64_t tiles, int heads, int kv_heads, int d) { return tiles * (heads + kv_heads) <= (d <= 64 ? 1536 : 768); }
+// (heads + key heads).  Heads of 64: 768: 54 and 48; 864: 78 and 70; 1024: 34 and 34 (16 x 197), 229 and 217 (4096); 1216: 68 and 67; 1280: 76 and 73 (8 x 512), 163 and 175
+// (2 x 2048); 1536: 112 and 117, 48 and 49; 1920: 137 and 142.  Heads of 32: 512: 22 and 16; 768: 33 and 30; 1280: 46 and 50; 1536: 74 and 81.  Heads of 65 to 128: 512: 44
+// and 40; 640: 82 and 75, 175 and 163; 760: 88 and 86; 768: 45 and 55 (16 x 197, 104 columns); 1024: 90 and 106.  (Two: dQ blocks of 128 queries.)
+inline bool packed_one_launch(int64_t tiles, int heads, int kv_heads, int d) { return tiles * (heads + kv_heads) <= (d <= 64 ? 1024 : 640); }
 
 // Steps of a tile's keys over all the heads that share them, and the first row that sees one.
 __host__ __device__ inline int walk_first(int causal, int tile) { return causal ? tile * kPackedTile : 0; }
