@@ -75,10 +75,13 @@ constexpr int kMostPieces = 512;
 // How many steps of a walk an item takes, and by how many the longest walk may exceed that without any being cut.  A launch lasts as long as its longest block,
 // and a key tile's walk is as long as the queries that see it times the heads that share it, so few keys and long walks leave the chip idle: walks
 // are cut to an equal share of all steps on the blocks that run at once: 256 of eight wavefronts, twice that for heads up to 64 (fp32 cuts a tile's
-// keys into eighths first).  Where the dQ blocks run in the same launch they fill what the longest items leave, so the share is a little longer, and it
-// is one of the blocks that they leave where that is a quarter or more.  Pieces pay for their places in the workspace and for the launch that joins them, as much
-// as five steps or so (fp32, whose steps take longer: 2).  Us of the whole backward, without pieces, in pieces of 8, of 4: 2 x 512 tokens, 4 heads of 64 over 2,
-// causal 44, 26, 16; 8 x 512, 8 over 8: 20, 20, 29; 700 + 300 + 100, 16 of 128 over 4: 95, 33, 43.
+// keys into eighths first).  Us of the whole backward without pieces, and with them: 2 x 512 tokens, 4 heads of 64 over 2, causal: 28 and 16; 700 + 300 + 100, 16 of 128 over 4: 96 and
+// 33; 2048, 16 of 128 over 1: 1028 and 93; fp32, 2 x 512, 8 of 64 over 1: 222 and 83.
+// Where the dQ blocks run in the same launch they fill what the longest items leave, so the share is 1.2 times as long (4096 tokens, 8 of 128 over 1: 152; 1.0 and
+// 1.4 times: 162 and 168), and it is one of the blocks that they leave where that is a quarter or more (700 + 300 + 100: 33; never: 39).  Pieces pay for their places in the workspace
+// and for the launch that joins them, as much as five steps (8 x 512, 8 of 64 over 8: 21; from none on 29; from twelve on, 2 x 512: 28 for 16), in fp32, whose steps take
+// longer, two (2 x 197, 4 of 64 over 2: 23; five: 32); none is shorter than four steps (2 x 512: 16; eight: 20; fp32, 2 x 197, two: 31), and a walk is cut from 5/4 of a share on
+// (700 + 300 + 100: 33; from 8/5 on: 41).
 struct Share { int steps, slack; };
 Share steps_an_item(const cephalo_packed_desc* d, int64_t tiles, int64_t steps) {
   const bool f32 = d->dtype == CEPHALO_F32, wide = d->head_dim > 64;
@@ -89,7 +92,7 @@ Share steps_an_item(const cephalo_packed_desc* d, int64_t tiles, int64_t steps) 
     share *= 1.2;
     if (left >= blocks / 4) share = std::max(share, (double)all / left);
   }
-  return {(int)std::min(std::max(std::ceil(share), 4.0), 1e9), 5};
+  return {(int)std::min(std::max(std::ceil(share), 4.0), 1e9), f32 ? 2 : 5};
 }
 }  // namespace
 
