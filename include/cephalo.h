@@ -348,7 +348,9 @@ int cephalo_op_attention_bwd(const cephalo_layer_desc* desc, const void* qkv, co
  * to no sample are neither read nor written, and neither are columns past a row's width.  Inside a sample a row that the causal
  * mask hides has a weight of zero, which in BF16 mode does not silence an infinity or a not-a-number: it can reach the rows
  * less than 128 away.  In F32 mode hidden rows are left out.
- * The forward holds for any scores that are finite in 32 bits, times log2(e) too. */
+ * The forward holds for any scores that are finite in 32 bits, times log2(e) too.  Scores, weights, statistics and sums are held in 32 bits; in BF16 mode what a matrix
+ * product takes is rounded to BF16 first: the weights before they meet the values or dO, dS before it meets the keys or queries (about 0.002 of a result's norm, where
+ * products in 32 bits leave 0.0016), and sum dO O takes O as it was stored. */
 typedef struct cephalo_packed_desc {
   int32_t heads, kv_heads;   /* heads is a multiple of kv_heads */
   int32_t head_dim;          /* up to 128, in BF16 mode a multiple of 8 */
@@ -365,7 +367,9 @@ typedef struct cephalo_packed_desc {
  * (not decreasing, inside [0, tokens]) is host memory, and so is `plan`, at least cephalo_packed_plan_bytes(samples, tokens)
  * bytes; the caller copies its first desc->plan_bytes bytes to the device, where the calls below take it.  Fills the desc's last fields.
  * The list holds how the work is divided (128 queries of a sample at a time; 128 keys and all or some of the queries that see them), so it goes
- * with the desc that it was made for.  The calls refuse what would pass the 2^32 threads of a launch: about 2^24 pairs of a head and 128 rows of a sample (or
+ * with the desc that it was made for, as that call left it: a desc that is planned again, or whose heads, head_dim, causal, dtype or tokens change, needs the new list, and each set of
+ * samples that is in use a desc of its own.  The calls cannot see which list they are given.  With another's, of plan_bytes bytes at least, they reach nothing outside the buffers' rows and the
+ * workspace, leave out what does not fit, and return CEPHALO_OK with results that mean nothing.  The calls refuse what would pass the 2^32 threads of a launch: about 2^24 pairs of a head and 128 rows of a sample (or
  * what it has below that), in F32 mode 2^20, with a head_dim above 96 2^21. */
 size_t cephalo_packed_plan_bytes(int32_t samples, int64_t tokens);
 int cephalo_packed_plan(cephalo_packed_desc* desc, int32_t samples, const int32_t* starts, void* plan, size_t plan_bytes);

@@ -510,7 +510,7 @@ __global__ void __launch_bounds__(256) packed_join_kernel(PackedArgs p, bf16* __
   const KeyItem e = p.joins[blockIdx.y];
   const int g = blockIdx.z, i = blockIdx.x * 256 + threadIdx.x, lane = i & 63, j = (i >> 6) % (D / 8), keys32 = i / (8 * D) % 4, which = i / (32 * D);
   const int t = e.tile * kPackedTile + keys32 * 32 + (lane & 31), d0 = 8 * j + 4 * (lane >> 5);
-  if (!rows_fit(p, e.first, e.rows, e.tile) || t >= e.rows || d0 >= p.d || e.slot < 0 || e.slot + e.pieces > p.slots) return;
+  if (!rows_fit(p, e.first, e.rows, e.tile) || t >= e.rows || d0 >= p.d || e.slot < 0 || e.pieces > p.slots - e.slot) return;
   const f32x4* part = reinterpret_cast<const f32x4*>(p.part) + ((size_t)e.slot * p.kv_heads + g) * (kPackedTile * D / 2) + i;
   f32x4 sum = {0.f, 0.f, 0.f, 0.f};
   for (int q = 0; q < e.pieces; ++q) sum += part[(size_t)q * p.kv_heads * (kPackedTile * D / 2)];

@@ -240,7 +240,7 @@ __global__ void __launch_bounds__(256) packed_f32_join_kernel(PackedArgs p, floa
   const KeyItem e = p.joins[blockIdx.y];
   const int g = blockIdx.z, width = packed_width(p.d), i = blockIdx.x * 256 + threadIdx.x, c = i % width, row = i / width % kPackedTile, which = i / (kPackedTile * width);
   const int t = e.tile * kPackedTile + row;
-  if (!rows_fit(p, e.first, e.rows, e.tile) || t >= e.rows || c >= p.d || e.slot < 0 || e.slot + e.pieces > p.slots) return;
+  if (!rows_fit(p, e.first, e.rows, e.tile) || t >= e.rows || c >= p.d || e.slot < 0 || e.pieces > p.slots - e.slot) return;
   const size_t place = 2 * (size_t)kPackedTile * width;
   const float* part = p.part + ((size_t)e.slot * p.kv_heads + g) * place + i;
   float sum = 0.f;
