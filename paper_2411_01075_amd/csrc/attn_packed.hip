@@ -37,8 +37,8 @@ template <int D> constexpr int kDkvWaves = D == 32 ? 3 : 2;
 // for each, and 32 exponentials a lane.  LDS gives 128 bytes a clock to four SIMDs, just what the products take, and the tiles' arrival is a quarter more.
 // A wavefront alone on its SIMD issues an instruction of the vector unit every 8 clocks, two together one every 4, so the exponentials have to run
 // under products: the next tile's scores are formed while this tile's exponentials run.  Against the attention of equal samples, which works on one tile at
-// a time, in TFLOP/s: 8192 tokens, 32 heads of 128, no mask 1078 -> 1138, causal 870 -> 1049; 32 heads of 64, causal 879 -> 949 (a large matrix
-// product of this library reaches 1340).
+// a time, in TFLOP/s: 8192 tokens, 32 heads of 128, no mask 1090 -> 1157, causal 1043 -> 1117; 32 heads of 64, causal 891 -> 938 (a large matrix
+// product of this library reaches 1354).
 __device__ __forceinline__ float halves_max(float v) {      // of lanes l and l ^ 32
   const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, v), __builtin_bit_cast(unsigned, v), false, false);
   const unsigned low = r[0], high = r[1];                // (values of their own: a bit cast of a vector's element takes the vector's first)
