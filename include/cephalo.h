@@ -370,7 +370,7 @@ typedef struct cephalo_packed_desc {
  * with the desc that it was made for, as that call left it: a desc that is planned again, or whose heads, head_dim, causal, dtype or tokens change, needs the new list, and each set of
  * samples that is in use a desc of its own.  The calls cannot see which list they are given.  With another's, of plan_bytes bytes at least, they reach nothing outside the buffers' rows and the
  * workspace, leave out what does not fit, and return CEPHALO_OK with results that mean nothing.  The calls refuse what would pass the 2^32 threads of a launch: about 2^24 pairs of a head and 128 rows of a sample (or
- * what it has below that), in F32 mode 2^20, with a head_dim above 96 2^21. */
+ * what it has below that), with a head_dim above 64 2^23 of a key head; in F32 mode 2^20, with a head_dim above 96 2^21. */
 size_t cephalo_packed_plan_bytes(int32_t samples, int64_t tokens);
 int cephalo_packed_plan(cephalo_packed_desc* desc, int32_t samples, const int32_t* starts, void* plan, size_t plan_bytes);
 

@@ -553,6 +553,16 @@ def test_both_ends_of_the_scale_with_ordinary_scores(dtype, heads, kv_heads, d, 
     assert zero < 1e-4 and w < 1e-2
 
 
+@pytest.mark.parametrize("dtype,heads,kv_heads,d,lengths", [("bf16", 4, 2, 32, [333, 100]), ("bf16", 4, 2, 64, [333, 100]), ("bf16", 4, 2, 104, [333, 100]), ("bf16", 40, 8, 64, FULLER),
+                                                            ("bf16", 32, 8, 128, FULL), ("f32", 4, 2, 64, [333, 100]), ("f32", 4, 2, 80, [333, 100])])
+def test_hidden_keys_with_scores_beyond_any_that_a_row_sees(dtype, heads, kv_heads, d, lengths):
+    """Every 17th key forty times as long: a row before it, which does not see it, would give it a weight that 32 bits do not hold."""
+    for causal in (True, False):
+        c = Packed(dtype, heads, kv_heads, d, causal, lengths, scale=1.0)
+        c.qkv[5::17, heads * d:(heads + kv_heads) * d] *= 40
+        _check_sharp(c)
+
+
 # ---- forms that the cases above do not reach ----------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("causal", [True, False])
@@ -669,3 +679,68 @@ def test_views_that_do_not_cover_the_rows_are_refused():
         with pytest.raises(C.CephaloError, match="expected"):
             bad()
     torch.cuda.synchronize()
+
+
+# ---- side by side and captured ------------------------------------------------------------------------------------------------
+
+def test_calls_on_two_streams_at_once():
+    """Different samples, a workspace and a plan of their own: what each gives is what it gives alone."""
+    cases = [Packed("bf16", 16, 4, 64, True, FULL, seed=1), Packed("bf16", 8, 2, 128, False, [257, 1, 120], seed=2)]
+    want = []
+    for c in cases:
+        c.forward(); c.backward()
+        torch.cuda.synchronize()
+        want.append([t.clone() for t in (c.O, c.lse, c.dqkv)])
+        for t in (c.O, c.lse, c.dqkv):
+            t.fill_(MARK)
+    streams = [torch.cuda.Stream() for _ in cases]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for c, s in zip(cases, streams):
+            c.forward(stream=s); c.backward(stream=s)
+    torch.cuda.synchronize()
+    for c, w in zip(cases, want):
+        assert all(torch.equal(a, b) for a, b in zip(w, (c.O, c.lse, c.dqkv)))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_the_operators_together_in_a_graph_with_the_program_s_work_between_replays(dtype):
+    """Rotary, attention, dropout and the way back; new inputs and new words at each replay, against the same calls made eagerly."""
+    heads, kv_heads, d, lengths, p, seed = 8, 2, 64, [130, 1, 77], 0.25, 5
+    c = Packed(dtype, heads, kv_heads, d, True, lengths)
+    rows, turned, back = c.rows, torch.empty_like(c.qkv), torch.empty_like(c.qkv)
+    positions = torch.stack([torch.arange(rows), torch.arange(rows) // 7], 1).to(torch.int32).cuda()
+    resid = torch.randn(rows, heads * d, device="cuda")
+    out, counter = torch.empty_like(resid), torch.zeros(1, dtype=torch.int64, device="cuda")
+    source, n = c.qkv.clone(), rows * heads * d
+    c.qkv = turned
+    dy = torch.randn(rows, heads * d, device="cuda")
+
+    def step():
+        turned.copy_(source)
+        C.cephalo_op_rotary_axes(LIB[dtype], turned, c.width, turned, c.width, positions, rows, [32, 32], heads + kv_heads, d)
+        c.forward()
+        C.cephalo_op_dropout_add(LIB[dtype], c.O, resid, out, n, p, seed, 0, counter)
+        C.cephalo_op_dropout_bwd(LIB[dtype], dy, c.dO, n, p, seed, 0, counter)
+        c.backward()
+        back.copy_(c.dqkv)
+        C.cephalo_op_rotary_axes(LIB[dtype], back, c.width, back, c.width, positions, rows, [32, 32], heads + kv_heads, d, inverse=True)
+
+    inputs, results = [torch.randn(rows, c.width, device="cuda").to(TORCH[dtype]) for _ in range(3)], []
+    for k, x in enumerate(inputs):
+        source.copy_(x); counter.fill_(800 * k)
+        step()
+        torch.cuda.synchronize()
+        results.append([t.clone() for t in (out, c.dO, back)])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for k in (0, 1, 2, 1, 0):
+        source.copy_(inputs[k]); counter.fill_(800 * k)
+        for t in (out, c.dO, back, c.O, c.lse, c.dqkv):
+            t.fill_(MARK)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(results[k], (out, c.dO, back)))
+        float((back.float() ** 2).sum())
+    assert not torch.equal(results[0][1] != 0, results[1][1] != 0)
